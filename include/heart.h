@@ -306,6 +306,79 @@ size_t heart_attn_workspace_bytes(const heart_shape *shape);
 size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
 
 /*
+ * Key/value cache in pages, for clips (or any sequences) that are generated chunk by chunk: the keys and values of a chunk
+ * of new tokens are written once, and the queries of that chunk and of later ones attend to all that is there.  Beside the
+ * paper, which attends inside one whole clip.
+ *
+ * A cache is n_pages pages of `page` tokens; element (page, head, token, d) of k lies k_stride[0] * page + k_stride[1] *
+ * head + k_stride[2] * token + d ELEMENTS behind `k` (v alike), so both [n_pages,H,page,D] and [n_pages,page,H,D]
+ * allocations, and a k and a v in one allocation, can be passed.  Pointers and strides (in bytes) are multiples of 16, token
+ * strides positive, page in {16, 32, 64, 128, 256}, D in {64, 128}.  H: key heads.
+ *   HEART_CACHE_BF16: elements are bf16; k_exp and v_exp are NULL.
+ *   HEART_CACHE_E4M3: elements are 8 bits (e4m3 as in the OCP 8-bit floating point specification: finite up to 448, no
+ *     infinities), and k_exp, v_exp uint8 [n_pages,H,page] (contiguous, 16-byte aligned) hold an exponent for each row of
+ *     D: an element stands for code * 2^(exp - 127).  A power of two makes reading exact (codes have 4 significant bits) and
+ *     leaves one rounding, to the nearest code, in writing.
+ * B sequences: page_table int32 [B,max_pages] names the pages of each in order, kv_len int32 [B] says how many tokens it
+ * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
+ * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
+ * call's tensors (NULL: each has T/B of them), and the last of them is at position kv_len[b]-1.  Tokens behind cu_q[B], and
+ * output rows of them, are left alone.
+ * Nothing that these arrays hold leaves the tensors: a position below 0 or from max_pages * page on, and a page outside
+ * [0, n_pages), is not written and reads as zeros.  Sequences may share pages that no call writes; of two new tokens
+ * at one place of the cache, either or a mixture is kept.
+ * T = 0 and N = 0 are valid and launch nothing.
+ */
+#define HEART_CACHE_BF16 0
+#define HEART_CACHE_E4M3 1
+typedef struct heart_cache {
+  int n_pages, page, H, D, type;
+  int B, max_pages;
+  long long k_stride[3], v_stride[3]; /* page, head, token */
+  void *k, *v;
+  unsigned char *k_exp, *v_exp;
+  const int *page_table, *kv_len;
+} heart_cache;
+
+/*
+ * Writes the keys and values of the new tokens.  k, v: bf16 [T,H,D], strides {token, head} in elements (multiples of 8),
+ * 16-byte aligned.  e4m3: exp is that of the smallest power of two, 2^-126 at least, under which the row's largest finite
+ * element is at most 448 (127 for a row of zeros); NaN and infinities become NaN.  Nothing else of the cache is touched.
+ */
+int heart_cache_write(const heart_cache *cache, int T, const void *k, const long long k_stride[2], const void *v,
+                      const long long v_stride[2], const int *cu_q, void *stream);
+
+/*
+ * Reads tokens 0 .. min(kv_len[b], N) - 1 of every sequence back as bf16 [B,H,N,D] with strides {batch, head, token} in
+ * elements (multiples of 8): what heart_pool_qk and heart_block_sparse_attn take.  Rows behind them are left as they were.
+ * Exact, except that values below 2^-126 (the smallest normal bf16) may be read as zero.
+ */
+int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k_stride[3], void *v,
+                     const long long v_stride[3], void *stream);
+
+/*
+ * Attention of the new tokens over the cache, which holds them already.  q, out: bf16 [T,Hq,D], strides {token, head} in
+ * elements (multiples of 8), 16-byte aligned; Hq a multiple of H, query heads hq of G = Hq / H read key head hq / G.  The
+ * query at position p of sequence b (the last new token: kv_len[b]-1) sees the keys lo <= j < hi,
+ *   causal = 0: hi = kv_len[b];  causal = n > 0: hi = min(kv_len[b], (p / n + 1) * n), whole blocks of n positions (1:
+ *     ordinary causal attention; the tokens of a latent frame: frame after frame), and no keys for p < 0;
+ *   window = 0: lo = 0;  window = w > 0: lo = max(0, hi - w).
+ * out = softmax(scale q.k) v over these; scale <= 0 means 1/sqrt(D); lse fp32 [Hq,T] contiguous or NULL: natural
+ * log-sum-exp of the scaled logits.  A query without keys gives zeros (lse = -inf).
+ * Precision as heart_block_sparse_attn: bf16 products, fp32 sums, logits scaled and exponentiated in fp32, weights rounded
+ * to bf16 for the second contraction (the row sum adds them unrounded).  Cached rows of 8 bits enter as the bf16 values
+ * they stand for.  Rows from kv_len on may hold anything.
+ * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
+ * B, H, D alone), or NULL.  With it the keys of few queries are divided over the chip, into parts that depend on all
+ * lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on
+ * entry and undefined on return; two calls that run concurrently must not share one.
+ */
+int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, const long long q_stride[2], const int *cu_q,
+                     int causal, int window, float scale, void *out, const long long o_stride[2], float *lse,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t heart_cache_attn_workspace_bytes(const heart_cache *cache, int T, int Hq);
+
+/*
  * Error-guided Budgeted Calibration (Sec. 4.3): offline, not on the serving path.
  *
  * heart_ebc_band_error: the frequency-weighted velocity error of Eq. 6 (bands and weights:

@@ -39,6 +39,21 @@ class HeartShape(ctypes.Structure):
     ]
 
 
+class HeartCache(ctypes.Structure):
+    """Mirror of `heart_cache` in include/heart.h."""
+
+    _fields_ = [
+        ("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("H", ctypes.c_int), ("D", ctypes.c_int), ("type", ctypes.c_int),
+        ("B", ctypes.c_int), ("max_pages", ctypes.c_int),
+        ("k_stride", ctypes.c_longlong * 3), ("v_stride", ctypes.c_longlong * 3),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+    ]
+
+
+HEART_CACHE_BF16, HEART_CACHE_E4M3 = 0, 1  # cache types (include/heart.h)
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -101,6 +116,15 @@ def load_library() -> ctypes.CDLL:
     lib.heart_scores_antidiag.restype = ci
     lib.heart_scores_antidiag_workspace_bytes.argtypes = [sp, ci]
     lib.heart_scores_antidiag_workspace_bytes.restype = ctypes.c_size_t
+    cp, ll = ctypes.POINTER(HeartCache), ctypes.POINTER(ctypes.c_longlong)
+    lib.heart_cache_write.argtypes = [cp, ci, vp, ll, vp, ll, vp, vp]
+    lib.heart_cache_write.restype = ci
+    lib.heart_cache_read.argtypes = [cp, ci, vp, ll, vp, ll, vp]
+    lib.heart_cache_read.restype = ci
+    lib.heart_cache_attn.argtypes = [cp, ci, ci, vp, ll, vp, ci, ci, cf, vp, ll, vp, vp, ctypes.c_size_t, vp]
+    lib.heart_cache_attn.restype = ci
+    lib.heart_cache_attn_workspace_bytes.argtypes = [cp, ci, ci]
+    lib.heart_cache_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.heart_last_error.restype = ctypes.c_char_p
     _lib = lib
     return lib
@@ -415,6 +439,66 @@ def heart_scores_antidiag(q, k, block: int, stride: int, scores=None, workspace=
     if rc:
         _check("heart_scores_antidiag", rc)
     return scores
+
+
+def heart_cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None):
+    """Writes the keys and values of new tokens (bf16 [T,H,D]) into the pages of their sequences.
+
+    k_cache, v_cache: [n_pages,H,page,D] views, bf16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages,H,page] (the rows'
+    exponents); page_table int32 [B,max_pages]; kv_len int32 [B]: tokens of each sequence, the new ones among them; cu_q
+    int32 [B+1]: where each sequence's new tokens begin (None: T/B each)."""
+    rc = _native().cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q, k_exp, v_exp, torch._C._cuda_getDevice(),
+                               _stream())
+    if rc:
+        _check("heart_cache_write", rc)
+
+
+def heart_cache_read(k_cache, v_cache, page_table, kv_len, k=None, v=None, n: Optional[int] = None, k_exp=None, v_exp=None):
+    """The first n cached tokens of every sequence as bf16 (k, v) [B,H,n,D], for heart_pool_qk and heart_block_sparse_attn.
+    Rows behind a sequence's last token are left as they are in k and v; without k and v they are zeros, and n is all
+    that the page table has room for unless it is given."""
+    native = _native()
+    if k is None or v is None:
+        if n is None:
+            n = (page_table.shape[1] * k_cache.shape[2]) if k is v else (v if k is None else k).shape[2]
+        shape = (page_table.shape[0], k_cache.shape[1], n, k_cache.shape[3])
+        k = torch.zeros(shape, dtype=torch.bfloat16, device=k_cache.device) if k is None else k
+        v = torch.zeros(shape, dtype=torch.bfloat16, device=k_cache.device) if v is None else v
+    if n is not None and n != k.shape[2]:
+        raise ValueError("k must hold n tokens")
+    rc = native.cache_read(k_cache, v_cache, page_table, kv_len, k_exp, v_exp, k, v, torch._C._cuda_getDevice(), _stream())
+    if rc:
+        _check("heart_cache_read", rc)
+    return k, v
+
+
+def heart_cache_attn_workspace_bytes(q, k_cache, page_table) -> int:
+    """Bytes of workspace for heart_cache_attn of q [T,Hq,D] (0 where it has no use for one)."""
+    c = HeartCache(H=k_cache.shape[1], D=k_cache.shape[3], B=page_table.shape[0])
+    return int(load_library().heart_cache_attn_workspace_bytes(ctypes.byref(c), int(q.shape[0]), int(q.shape[1])))
+
+
+def heart_cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None, causal: int = 1,
+                     window: int = 0, scale: float = 0.0, out=None, lse=None, workspace="auto"):
+    """Attention of the new tokens' queries (bf16 [T,Hq,D]) over the cache, which holds their keys and values already (the
+    cache's arguments: heart_cache_write); returns bf16 out like q.
+
+    causal: 0 a query sees the whole sequence, n > 0 the blocks of n positions up to its own; window: only the last so
+    many of these keys (0: all).  lse: fp32 [Hq,T] or None.  workspace: a GPU tensor of at least
+    heart_cache_attn_workspace_bytes bytes (the keys of few queries are then divided over the chip), None, or "auto" (a
+    fresh tensor from torch's allocator)."""
+    native = _native()
+    if out is None:
+        out = torch.empty_like(q)
+    if isinstance(workspace, str):
+        if workspace != "auto":
+            raise ValueError("workspace must be a tensor, None or 'auto'")
+        workspace = torch.empty(heart_cache_attn_workspace_bytes(q, k_cache, page_table), dtype=torch.uint8, device=q.device)
+    rc = native.cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q, k_exp, v_exp, causal, window, scale, out, lse,
+                           workspace, torch._C._cuda_getDevice(), _stream())
+    if rc:
+        _check("heart_cache_attn", rc)
+    return out
 
 
 def heart_ebc_workspace_bytes(C: int, T: int, Y: int, X: int) -> int:

@@ -310,6 +310,114 @@ int heart_scores_antidiag(const heart_shape *shape, const void *q, const void *k
                          (hipStream_t)stream);
 }
 
+// what every call on a cache needs
+static int check_cache(const heart_cache *c, const char *fn) {
+  if (!c) return fail(HEART_EINVAL, "%s: cache is NULL", fn);
+  if (c->n_pages <= 0 || c->H <= 0 || c->B <= 0 || c->max_pages <= 0)
+    return fail(HEART_EINVAL, "%s: n_pages, H, B, max_pages must be positive (got %d, %d, %d, %d)", fn, c->n_pages, c->H,
+                c->B, c->max_pages);
+  if (c->D != 64 && c->D != 128) return fail(HEART_EUNSUPPORTED, "%s: D must be 64 or 128 (got %d)", fn, c->D);
+  if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)) != 0)
+    return fail(HEART_EUNSUPPORTED, "%s: page must be 16, 32, 64, 128 or 256 (got %d)", fn, c->page);
+  if (c->type != HEART_CACHE_BF16 && c->type != HEART_CACHE_E4M3)
+    return fail(HEART_EINVAL, "%s: unknown cache type %d", fn, c->type);
+  const bool e4m3 = c->type == HEART_CACHE_E4M3;
+  if (!c->k || !c->v || !c->page_table || !c->kv_len || (e4m3 && (!c->k_exp || !c->v_exp)))
+    return fail(HEART_EINVAL, "%s: NULL pointer in the cache", fn);
+  if (!e4m3 && (c->k_exp || c->v_exp)) return fail(HEART_EINVAL, "%s: a bf16 cache has no exponents", fn);
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_exp) || !aligned16(c->v_exp))
+    return fail(HEART_EUNSUPPORTED, "%s: the cache must be 16-byte aligned", fn);
+  const int step = e4m3 ? 16 : 8;
+  for (const long long *s : {c->k_stride, c->v_stride}) {
+    if (s[0] % step != 0 || s[1] % step != 0 || s[2] % step != 0 || s[2] <= 0)
+      return fail(HEART_EUNSUPPORTED, "%s: cache strides must be multiples of 16 bytes, token strides > 0", fn);
+    if (s[2] > (1ll << 22))  // (a page is addressed through 32-bit offsets)
+      return fail(HEART_EUNSUPPORTED, "%s: cache token strides must not exceed 2^22 elements", fn);
+  }
+  if (c->max_pages > 0x7fffffff / c->page)
+    return fail(HEART_EUNSUPPORTED, "%s: max_pages * page must stay below 2^31", fn);
+  return HEART_OK;
+}
+
+// strides of a bf16 tensor of the call
+static bool chunk_strides_ok(const long long *s, int n) {
+  for (int i = 0; i < n; ++i)
+    if (s[i] % 8 != 0) return false;
+  return true;
+}
+
+static int check_tokens(const heart_cache *c, int T, const int *cu_q, const char *fn) {
+  if (T < 0) return fail(HEART_EINVAL, "%s: T must not be negative (got %d)", fn, T);
+  if (T > (1 << 30)) return fail(HEART_EUNSUPPORTED, "%s: T must not exceed 2^30 (got %d)", fn, T);
+  if (!cu_q && T % c->B != 0)
+    return fail(HEART_EINVAL, "%s: without cu_q, T must be a multiple of B (got %d, %d)", fn, T, c->B);
+  return HEART_OK;
+}
+
+int heart_cache_write(const heart_cache *cache, int T, const void *k, const long long k_stride[2], const void *v,
+                      const long long v_stride[2], const int *cu_q, void *stream) {
+  clear_error();
+  const char *fn = "heart_cache_write";
+  if (int rc = check_cache(cache, fn)) return rc;
+  if (int rc = check_tokens(cache, T, cu_q, fn)) return rc;
+  if (!k_stride || !v_stride) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  if (T == 0) return HEART_OK;
+  if (!k || !v) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  if (!aligned16(k) || !aligned16(v)) return fail(HEART_EUNSUPPORTED, "%s: k and v must be 16-byte aligned", fn);
+  if (!chunk_strides_ok(k_stride, 2) || !chunk_strides_ok(v_stride, 2))
+    return fail(HEART_EUNSUPPORTED, "%s: strides must be multiples of 8 elements", fn);
+  return launch_cache_write(*cache, T, k, k_stride, v, v_stride, cu_q, (hipStream_t)stream);
+}
+
+int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k_stride[3], void *v,
+                     const long long v_stride[3], void *stream) {
+  clear_error();
+  const char *fn = "heart_cache_read";
+  if (int rc = check_cache(cache, fn)) return rc;
+  if (N < 0) return fail(HEART_EINVAL, "%s: N must not be negative (got %d)", fn, N);
+  if (!k_stride || !v_stride) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  if (N == 0) return HEART_OK;
+  if (!k || !v) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  if (!aligned16(k) || !aligned16(v)) return fail(HEART_EUNSUPPORTED, "%s: k and v must be 16-byte aligned", fn);
+  if (!chunk_strides_ok(k_stride, 3) || !chunk_strides_ok(v_stride, 3))
+    return fail(HEART_EUNSUPPORTED, "%s: strides must be multiples of 8 elements", fn);
+  return launch_cache_read(*cache, N, k, k_stride, v, v_stride, (hipStream_t)stream);
+}
+
+int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, const long long q_stride[2], const int *cu_q,
+                     int causal, int window, float scale, void *out, const long long o_stride[2], float *lse,
+                     void *workspace, size_t workspace_bytes, void *stream) {
+  clear_error();
+  const char *fn = "heart_cache_attn";
+  if (int rc = check_cache(cache, fn)) return rc;
+  if (int rc = check_tokens(cache, T, cu_q, fn)) return rc;
+  if (Hq <= 0 || Hq % cache->H != 0)
+    return fail(HEART_EINVAL, "%s: Hq must be a positive multiple of the cache's heads (got %d, %d)", fn, Hq, cache->H);
+  if (causal < 0 || window < 0)
+    return fail(HEART_EINVAL, "%s: causal and window must not be negative (got %d, %d)", fn, causal, window);
+  if (!q_stride || !o_stride) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  if (T == 0) return HEART_OK;
+  if (!q || !out) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  if (!aligned16(q) || !aligned16(out)) return fail(HEART_EUNSUPPORTED, "%s: q and out must be 16-byte aligned", fn);
+  if (!chunk_strides_ok(q_stride, 2) || !chunk_strides_ok(o_stride, 2))
+    return fail(HEART_EUNSUPPORTED, "%s: strides must be multiples of 8 elements", fn);
+  if ((long long)T * Hq > 0x3fffffffLL || ((long long)T + cache->B) * Hq > 0x7fffffffLL)
+    return fail(HEART_EUNSUPPORTED, "%s: T * Hq must not exceed 2^30 (got %d, %d)", fn, T, Hq);
+  if (workspace) {
+    if (!aligned16(workspace)) return fail(HEART_EUNSUPPORTED, "%s: workspace must be 16-byte aligned", fn);
+    const size_t need = heart_cache_attn_workspace_bytes(cache, T, Hq);
+    if (workspace_bytes < need)
+      return fail(HEART_EINVAL, "%s: workspace of %zu bytes, need %zu", fn, workspace_bytes, need);
+  }
+  return launch_cache_attn(*cache, T, Hq, q, q_stride, cu_q, causal, window, scale, out, o_stride, lse, workspace,
+                           (hipStream_t)stream);
+}
+
+size_t heart_cache_attn_workspace_bytes(const heart_cache *c, int T, int Hq) {
+  if (!c || c->B <= 0 || c->H <= 0 || (c->D != 64 && c->D != 128) || T <= 0 || Hq <= 0 || Hq % c->H != 0) return 0;
+  return cache_attn_workspace_bytes(c->B, c->H, c->D, T, Hq);
+}
+
 int heart_ebc_band_error(long long C, int T, int Y, int X, const float *err, const float *dense,
                          const double *weights4_host, double epsilon, void *workspace,
                          size_t workspace_bytes, double *out6, void *stream) {

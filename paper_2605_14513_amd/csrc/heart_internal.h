@@ -303,6 +303,15 @@ int launch_antidiag(const heart_shape &s, const void *q, const void *k, int stri
                     const unsigned char *refresh, float *scores, float *workspace, hipStream_t st);
 size_t antidiag_workspace_bytes(const heart_shape &s, int stride);
 
+int launch_cache_write(const heart_cache &c, int T, const void *k, const long long ks[2], const void *v,
+                       const long long vs[2], const int *cu_q, hipStream_t st);
+int launch_cache_read(const heart_cache &c, int N, void *k, const long long ks[3], void *v, const long long vs[3],
+                      hipStream_t st);
+int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const long long qs[2], const int *cu_q, int causal,
+                      int window, float scale, void *out, const long long os[2], float *lse, void *workspace,
+                      hipStream_t st);
+size_t cache_attn_workspace_bytes(int B, int H, int D, int T, int Hq);
+
 int launch_ebc_band_error(long long C, int T, int Y, int X, const float *err, const float *dense,
                           const double *w, double epsilon, double *ws, double *out,
                           hipStream_t st);

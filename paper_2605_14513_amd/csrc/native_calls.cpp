@@ -29,6 +29,7 @@ const char *torch_name(at::ScalarType t) {
     case at::kDouble: return "torch.float64";
     case at::kInt: return "torch.int32";
     case at::kByte: return "torch.uint8";
+    case at::kFloat8_e4m3fn: return "torch.float8_e4m3fn";
     default: return c10::toString(t);
   }
 }
@@ -116,6 +117,10 @@ int integer32(PyObject *o) {
 long block_of(PyObject *o) {
   if (!PyIndex_Check(o)) type_error("block must be an integer");
   return integer(o);
+}
+int whole32(PyObject *o, const char *name) {
+  if (!PyIndex_Check(o)) type_error(std::string(name) + " must be an integer");
+  return integer32(o);
 }
 double real(PyObject *o) {
   const double v = PyFloat_AsDouble(o);
@@ -259,6 +264,153 @@ PyObject *scores_antidiag(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the paged key/value cache ----------------------------------------------------------------
+
+// `t` on the device that the call runs on
+const Tensor &on(PyObject *o, const char *name, long device) {
+  const Tensor &t = some(o, name);
+  if (!t.is_cuda()) type_error(std::string(name) + " must be a GPU tensor");
+  if (t.device().index() != device) value_error(std::string(name) + " must be on the current device");
+  return t;
+}
+void check_type(const Tensor &t, at::ScalarType type, const char *name) {
+  if (t.scalar_type() != type)
+    type_error(std::string(name) + " must have dtype " + torch_name(type) + ", got " + torch_name(t.scalar_type()));
+}
+const int *ints(PyObject *o, const char *name, long device, Sizes want, const char *msg) {
+  const Tensor &t = on(o, name, device);
+  check_type(t, at::kInt, name);
+  if (t.sizes() != want) value_error(msg);
+  if (!t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+  return static_cast<const int *>(t.data_ptr());
+}
+// strides of all axes but the last, which is contiguous; an axis of one element is not walked
+void outer_strides(const Tensor &t, const char *name, int n, long long *out) {
+  if (t.stride(n) != 1) value_error(std::string(name) + " must have a contiguous D axis");
+  for (int i = 0; i < n; ++i) out[i] = t.size(i) == 1 ? 0 : t.stride(i);
+}
+// k_cache, v_cache, page_table, kv_len; k_exp, v_exp
+heart_cache cache_of(PyObject *const *a, PyObject *const *exps, long device) {
+  const Tensor &k = on(a[0], "k_cache", device), &v = on(a[1], "v_cache", device), &table = on(a[2], "page_table", device);
+  if (k.dim() != 4 || v.sizes() != k.sizes()) value_error("k_cache and v_cache must both be [n_pages,H,page,D]");
+  const at::ScalarType type = k.scalar_type();
+  if (type != at::kBFloat16 && type != at::kFloat8_e4m3fn)
+    type_error(std::string("k_cache must have dtype torch.bfloat16 or torch.float8_e4m3fn, got ") + torch_name(type));
+  check_type(v, type, "v_cache");
+  if (table.dim() != 2) value_error("page_table must be [B,max_pages]");
+  for (int i = 0; i < 4; ++i)
+    if (k.size(i) > INT_MAX) value_error("k_cache is too large");
+  if (table.size(0) > INT_MAX || table.size(1) > INT_MAX) value_error("page_table is too large");
+  heart_cache c{};
+  c.n_pages = (int)k.size(0), c.H = (int)k.size(1), c.page = (int)k.size(2), c.D = (int)k.size(3);
+  c.type = type == at::kBFloat16 ? HEART_CACHE_BF16 : HEART_CACHE_E4M3;
+  c.B = (int)table.size(0), c.max_pages = (int)table.size(1);
+  outer_strides(k, "k_cache", 3, c.k_stride);
+  outer_strides(v, "v_cache", 3, c.v_stride);
+  c.k = k.data_ptr(), c.v = v.data_ptr();
+  c.page_table = ints(a[2], "page_table", device, table.sizes(), "");
+  const int64_t lens[1] = {c.B};
+  c.kv_len = ints(a[3], "kv_len", device, lens, "kv_len must be [B]");
+  const char *names[2] = {"k_exp", "v_exp"};
+  unsigned char **to[2] = {&c.k_exp, &c.v_exp};
+  for (int i = 0; i < 2; ++i) {
+    if (c.type == HEART_CACHE_BF16) {
+      if (exps[i] != Py_None) value_error(std::string(names[i]) + ": a bf16 cache has no exponents");
+      continue;
+    }
+    const Tensor &e = on(exps[i], names[i], device);
+    check_type(e, at::kByte, names[i]);
+    if (e.sizes() != k.sizes().slice(0, 3)) value_error(std::string(names[i]) + " must be [n_pages,H,page]");
+    if (!e.is_contiguous()) value_error(std::string(names[i]) + " must be contiguous");
+    *to[i] = static_cast<unsigned char *>(e.data_ptr());
+  }
+  return c;
+}
+// bf16 [T,heads,D] of the call; heads = 0: any number
+const Tensor &chunk(PyObject *o, const char *name, long device, const heart_cache &c, int64_t heads, long long strides[2]) {
+  const Tensor &t = on(o, name, device);
+  check_type(t, at::kBFloat16, name);
+  if (t.dim() != 3 || t.size(2) != c.D || (heads && t.size(1) != heads))
+    value_error(std::string(name) + (heads ? " must be [T,H,D] with the cache's H and D" : " must be [T,Hq,D] with the cache's D"));
+  if (t.size(0) > INT_MAX || t.size(1) > INT_MAX) value_error(std::string(name) + " is too large");
+  outer_strides(t, name, 2, strides);
+  return t;
+}
+const int *cu_of(PyObject *o, long device, const heart_cache &c) {
+  const int64_t ends[1] = {(int64_t)c.B + 1};
+  return o == Py_None ? nullptr : ints(o, "cu_q", device, ends, "cu_q must be [B+1]");
+}
+
+PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  check_count(n, 11);
+  const long device = integer(a[9]);
+  const heart_cache c = cache_of(a + 2, a + 7, device);
+  long long ks[2], vs[2];
+  const Tensor &k = chunk(a[0], "k", device, c, c.H, ks), &v = chunk(a[1], "v", device, c, c.H, vs);
+  if (k.size(0) != v.size(0)) value_error("k and v must have the same shape");
+  const int *cu = cu_of(a[6], device, c);
+  const void *kp = k.data_ptr(), *vp = v.data_ptr();
+  const int T = (int)k.size(0);
+  void *st = handle(a[10]);
+  return call([&] { return heart_cache_write(&c, T, kp, ks, vp, vs, cu, st); });
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  check_count(n, 10);
+  const long device = integer(a[8]);
+  const heart_cache c = cache_of(a, a + 4, device);
+  const Tensor &k = on(a[6], "k", device), &v = on(a[7], "v", device);
+  check_type(k, at::kBFloat16, "k");
+  check_type(v, at::kBFloat16, "v");
+  if (k.dim() != 4 || k.size(0) != c.B || k.size(1) != c.H || k.size(3) != c.D || k.sizes() != v.sizes())
+    value_error("k and v must both be [B,H,N,D] with the B of page_table and the cache's H and D");
+  if (k.size(2) > INT_MAX) value_error("k is too large");
+  long long ks[3], vs[3];
+  outer_strides(k, "k", 3, ks);
+  outer_strides(v, "v", 3, vs);
+  void *kp = k.data_ptr(), *vp = v.data_ptr(), *st = handle(a[9]);
+  const int N = (int)k.size(2);
+  return call([&] { return heart_cache_read(&c, N, kp, ks, vp, vs, st); });
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject *cache_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  check_count(n, 16);
+  const long device = integer(a[14]);
+  const heart_cache c = cache_of(a + 1, a + 6, device);
+  long long qs[2], os[2];
+  const Tensor &q = chunk(a[0], "q", device, c, 0, qs);
+  const Tensor &out = chunk(a[11], "out", device, c, 0, os);
+  if (out.sizes() != q.sizes()) value_error("out must have the shape of q");
+  const int *cu = cu_of(a[5], device, c);
+  const int causal = whole32(a[8], "causal"), window = whole32(a[9], "window");
+  const float scale = (float)real(a[10]);
+  float *lse = nullptr;
+  if (a[12] != Py_None) {
+    const Tensor &l = on(a[12], "lse", device);
+    check_type(l, at::kFloat, "lse");
+    const int64_t want[2] = {q.size(1), q.size(0)};
+    if (l.sizes() != Sizes(want)) value_error("lse must be [Hq,T]");
+    if (!l.is_contiguous()) value_error("lse must be contiguous");
+    lse = static_cast<float *>(l.data_ptr());
+  }
+  size_t ws_bytes = 0;
+  void *ws = nullptr;
+  if (a[13] != Py_None) {
+    on(a[13], "workspace", device);
+    ws = scratch(a[13], &ws_bytes);
+  }
+  const void *qp = q.data_ptr();
+  void *op = out.data_ptr(), *st = handle(a[15]);
+  const int T = (int)q.size(0), Hq = (int)q.size(1);
+  return call([&] { return heart_cache_attn(&c, T, Hq, qp, qs, cu, causal, window, scale, op, os, lse, ws, ws_bytes, st); });
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject *ebc_band_error(PyObject *, PyObject *const *a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   check_count(n, 10);
@@ -293,6 +445,9 @@ PyMethodDef methods[] = {
     {"block_sparse_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_sparse_attn)), METH_FASTCALL, nullptr},
     {"scores_antidiag", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(scores_antidiag)), METH_FASTCALL, nullptr},
     {"ebc_band_error", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(ebc_band_error)), METH_FASTCALL, nullptr},
+    {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_write)), METH_FASTCALL, nullptr},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, nullptr},
+    {"cache_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attn)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", HEART_TORCH, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
