@@ -24,127 +24,18 @@
 //     time than the products take.
 #include <type_traits>
 
-#include "cache_device.h"
+#include "cache_attn_device.h"
 
 namespace heart {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-typedef __attribute__((ext_vector_type(2))) float f32x2_t;
-typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-
-union Frag8 {
-  u32x4_t u;
-  bf16x8_t v;
-};
-
-static __device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
-  f32x2_t f = {lo, hi};
-  bf16x2_t b = __builtin_convertvector(f, bf16x2_t);
-  return __builtin_bit_cast(uint32_t, b);
-}
 
 constexpr int kTile = 128;      // rows of a workgroup
 constexpr int kStage = 64;      // keys of a stage
 constexpr int kPlaces = 512;    // places for workgroups: two a CU
 constexpr int kMinStages = 4;   // fewest stages of a part
-constexpr int kSplitSeqs = 256; // most sequences of a call whose keys are divided
 
 // floats of one wavefront's part: accumulators, reference exponent and row sum of every lane
 template <int D>
 constexpr int kPartFloats = 64 * (D / 2) + 128;
-
-// K or V of the cache
-struct CacheTensor {
-  const uint8_t *p, *exp;
-  long long page, head;  // bytes
-  uint32_t row;          // bytes between tokens
-};
-struct AttnCall {
-  CacheTensor k, v;
-  CacheSeqs s;
-  const uint16_t *q;
-  uint16_t *out;
-  float *lse;
-  long long qt, qh, ot, oh;  // elements
-  int H, G, causal, window;
-  float scale_log2e;
-  int4 *items;  // (divided keys) of each item: number of its first part, parts, parts' distance
-  float *part;
-};
-
-// One sequence as a kernel sees it.
-struct Seq {
-  int first, n, len;  // first new token, new tokens, cached tokens that there is room for
-  int pos0;           // position of the first new token (may be negative)
-  int tiles;
-};
-__device__ __forceinline__ Seq seq_of(const AttnCall &c, int b) {
-  Seq s;
-  s.first = c.s.cu ? c.s.cu[b] : b * c.s.per;
-  const int end = c.s.cu ? c.s.cu[b + 1] : s.first + c.s.per;
-  // (token numbers outside the call's tensors: no tokens)
-  s.n = s.first >= 0 && end > s.first && end <= c.s.T ? end - s.first : 0;
-  const int kv = min(max(c.s.kv_len[b], 0), 0x7fffffff - 0x100);
-  s.pos0 = kv - s.n;
-  s.len = min(kv, c.s.cap);
-  s.tiles = (s.n * c.G + kTile - 1) / kTile;
-  return s;
-}
-// Keys lo .. hi - 1 that the query at position p sees.
-__device__ __forceinline__ void seen_by(const AttnCall &c, const Seq &s, int p, int &lo, int &hi) {
-  hi = s.len;
-  if (c.causal) {
-    const uint32_t end = (uint32_t)max(p, 0) / (uint32_t)c.causal * (uint32_t)c.causal + (uint32_t)c.causal;  // < 2^32
-    hi = p < 0 ? 0 : (int)min(end, (uint32_t)s.len);
-  }
-  lo = c.window ? max(0, hi - c.window) : 0;
-}
-// Stages that a tile of the sequence walks through at most (what the division of the keys goes by).
-__device__ __forceinline__ int stages_of(const AttnCall &c, const Seq &s) {
-  int st = (s.len + kStage - 1) / kStage;
-  if (c.window) {
-    const long long span = (long long)c.window + kTile / c.G + max(c.causal, 1);
-    st = (int)min((long long)st, span / kStage + 2);
-  }
-  return max(st, 1);
-}
-// Tiles are numbered so that a number's sequence can be found from the token ranges: those of sequence b start at
-// first G / 128 + b, which leaves room for a short last tile of each.
-__device__ __forceinline__ int tile_start(const AttnCall &c, int b) {
-  const int first = c.s.cu ? c.s.cu[b] : b * c.s.per;
-  return (int)((unsigned)max(first, 0) * (unsigned)c.G / kTile) + b;
-}
-// The last sequence whose tiles start at or before `tile`.
-__device__ __forceinline__ int seq_of_tile(const AttnCall &c, int tile, int lane) {
-  if (!c.s.cu) {
-    // (b (per G / 128 + 1) rounded down: one division finds b or its neighbour)
-    int b = min((int)((long long)tile * kTile / ((long long)c.s.per * c.G + kTile)), c.s.B - 1);
-    while (b > 0 && tile_start(c, b) > tile) --b;
-    while (b + 1 < c.s.B && tile_start(c, b + 1) <= tile) ++b;
-    return b;
-  }
-  int lo = 0, n = c.s.B;  // (starts grow with b: 64 places at a time)
-  while (n > 1) {
-    const int step = (n + 63) / 64, at = lo + lane * step;
-    const bool before = lane * step < n && tile_start(c, at) <= tile;
-    const int k = max(__popcll(__ballot(before)) - 1, 0);
-    lo += k * step;
-    n = min(step, n - k * step);
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
-}
-
-// What a workgroup works on.
-struct Work {
-  int b, h, m;            // sequence, key head, tile
-  int part, parts, step;  // (divided keys) part of the tile's stages, their number, distance of their numbers
-  int slot;               // number of the part
-};
 
 // (divided keys) The part of workgroup w: the sequences' parts one after the other; of a sequence, head after head, parts,
 // tiles, so that workgroups that read the same keys are neighbours.  Parts have at most L stages, the least L with which
@@ -160,8 +51,8 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
     st[j] = 1;
     if (j * 64 < c.s.B && b < c.s.B) {
       const Seq s = seq_of(c, b);
-      wgs[j] = s.tiles * c.H;
-      st[j] = stages_of(c, s);
+      wgs[j] = tiles_of<kTile>(c, s) * c.H;
+      st[j] = stages_of<kTile, kStage>(c, s);
       most = max(most, wgs[j] ? st[j] : 1);
     }
   }
@@ -205,15 +96,6 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
   return true;
 }
 
-// Row r of a tile's sequence: where its query, output and log-sum-exp are.
-struct Row {
-  int token, head;
-};
-__device__ __forceinline__ Row row_of(const AttnCall &c, const Seq &s, int h, int r) {
-  const int i = (int)((unsigned)r / (unsigned)c.G);
-  return Row{s.first + i, h * c.G + r - i * c.G};
-}
-
 template <int D, bool kCodes, bool kSplit>
 __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   constexpr int DT = D / 32;             // 32-wide d tiles of the output
@@ -248,14 +130,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   } else {
     const int tile = (int)(blockIdx.x / (unsigned)c.H);
     wk.h = (int)(blockIdx.x % (unsigned)c.H);
-    wk.b = seq_of_tile(c, tile, lane);
-    wk.m = tile - tile_start(c, wk.b);
+    wk.b = seq_of_tile<kTile>(c, tile, lane);
+    wk.m = tile - tile_start<kTile>(c, wk.b);
   }
   wk.b = __builtin_amdgcn_readfirstlane(wk.b);
   const Seq s = seq_of(c, wk.b);
+  const int tiles = tiles_of<kTile>(c, s);
   if (!kSplit) wk.m = __builtin_amdgcn_readfirstlane(wk.m);
-  if (wk.m < 0 || wk.m >= s.tiles) return;
-  if (!kSplit) wk.m = s.tiles - 1 - wk.m;  // (later tiles see more keys: first)
+  if (wk.m < 0 || wk.m >= tiles) return;
+  if (!kSplit) wk.m = tiles - 1 - wk.m;  // (later tiles see more keys: first)
   const int rows = s.n * c.G, r0 = wk.m * kTile;
   int lo, hi, first_key, end_key, ignore;
   seen_by(c, s, s.pos0 + r0 / c.G, first_key, ignore);
@@ -266,7 +149,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     const int per = max((n_stage + wk.parts - 1) / wk.parts, 1);
     parts = max((n_stage + per - 1) / per, 1);
     if (wk.part == 0 && t == 0)
-      c.items[(long long)(tile_start(c, wk.b) + wk.m) * c.H + wk.h] = int4{wk.slot, parts, wk.step, 0};
+      c.items[(long long)(tile_start<kTile>(c, wk.b) + wk.m) * c.H + wk.h] = int4{wk.slot, parts, wk.step, 0};
     if (wk.part >= parts) return;
     stage0 += wk.part * per;
     n_stage = min(per, n_stage - wk.part * per);
@@ -701,10 +584,10 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
   const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
   const int wave = (int)(blockIdx.x % 4), item = (int)(blockIdx.x / 4);
   const int tile = item / c.H, h = item % c.H;
-  const int b = seq_of_tile(c, tile, lane), m = __builtin_amdgcn_readfirstlane(tile - tile_start(c, b));
+  const int b = seq_of_tile<kTile>(c, tile, lane), m = __builtin_amdgcn_readfirstlane(tile - tile_start<kTile>(c, b));
   const Seq s = seq_of(c, b);
   const int rows = s.n * c.G, row = m * kTile + wave * 32 + l32;
-  if (m < 0 || m >= s.tiles || m * kTile + wave * 32 >= rows) return;
+  if (m < 0 || m >= tiles_of<kTile>(c, s) || m * kTile + wave * 32 >= rows) return;
   const int4 it = c.items[item];
   if (it.y <= 1) return;
   float ref = ninf, l = 0.f;
@@ -760,11 +643,11 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
   }
 }
 
-// Tiles of a call at most, of all heads; divided keys pay where they are fewer than the places.
-static long long most_items(int B, int H, int T, int Hq) { return ((long long)T * (Hq / H) / kTile + B) * H; }
-static bool divides(int B, int H, int T, int Hq) { return B <= kSplitSeqs && most_items(B, H, T, Hq) < kPlaces; }
+// Divided keys pay where there are fewer tiles than places.
+static bool divides(int B, int H, int T, int Hq) { return B <= kSplitSeqs && most_items(kTile, B, H, T, Hq) < kPlaces; }
 
 size_t cache_attn_workspace_bytes(int B, int H, int D, int T, int Hq) {
+  if (cache_attn_few(B, H, T, Hq)) return cache_attn_few_workspace_bytes(B, H, D, T, Hq);
   if (!divides(B, H, T, Hq)) return 0;
   const size_t part = D == 128 ? kPartFloats<128> : kPartFloats<64>;
   return kPlaces * (sizeof(int4) + 4 * part * sizeof(float));
@@ -805,10 +688,11 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   a.qt = qs[0], a.qh = qs[1], a.ot = os[0], a.oh = os[1];
   a.H = c.H, a.G = Hq / c.H, a.causal = causal, a.window = window;
   a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.D)) * 1.4426950408889634f;
+  if (cache_attn_few(c.B, c.H, T, Hq)) return launch_cache_attn_few(c, T, Hq, a, workspace, st);
   const bool split = workspace && divides(c.B, c.H, T, Hq);
   a.items = (int4 *)workspace;
   a.part = split ? (float *)(a.items + kPlaces) : nullptr;
-  const long long items = most_items(c.B, c.H, T, Hq);
+  const long long items = most_items(kTile, c.B, c.H, T, Hq);
   if (items > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   if (c.D == 128) return codes ? launch_t<128, true>(a, split, items, st) : launch_t<128, false>(a, split, items, st);
   return codes ? launch_t<64, true>(a, split, items, st) : launch_t<64, false>(a, split, items, st);

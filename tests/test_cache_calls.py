@@ -102,9 +102,9 @@ def test_no_tokens_launch_nothing(lib):
 
 def test_workspace_sizes(lib):
     size = lambda T, Hq, **kw: lib.heart_cache_attn_workspace_bytes(ctypes.byref(cache(**kw)), T, Hq)  # noqa: E731
-    part = lambda D: 4 * (64 * (D // 2) + 128) * 4  # noqa: E731  (four wavefronts' accumulators, reference and sum)
-    assert size(3, 4) >= 512 * part(128) and size(3, 4, D=64) >= 512 * part(64)
-    assert size(3, 4) == size(6, 2)  # (a function of what divides the call, not of its tokens)
+    # room for parts of the keys, of few rows a key head and of more; a function of B, H, D, T, Hq alone
+    assert size(3, 4) > 0 and size(300, 4) > 0 and size(3, 4, D=64) < size(3, 4) and size(300, 4, D=64) < size(300, 4)
+    assert size(3, 4) == size(3, 4, n_pages=1, page=64, max_pages=1000, type=1, k_exp=F, v_exp=F)
     assert size(300000, 4) == 0      # (enough queries without division)
     assert size(0, 4) == size(3, 3) == size(3, 0) == size(3, 4, D=96) == size(3, 4, B=0) == 0
 
