@@ -1432,7 +1432,7 @@ __global__ __launch_bounds__(BLK * 2, HEART_ATTN_OCC) void attn_kernel(
 
 // A mark that no other call has (kMarkCount: its low bits are zero): counted from a place that the clock and the address space
 // of the process choose.
-static unsigned long long call_mark() {
+unsigned long long call_mark() {
   static std::atomic<unsigned long long> next{0};
   unsigned long long m = next.load(std::memory_order_relaxed);
   if (m == 0) {

@@ -678,7 +678,7 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
                       hipStream_t st) {
   const bool codes = c.type == HEART_CACHE_E4M3;
   const long long eb = codes ? 1 : 2;
-  AttnCall a;
+  AttnCall a{};
   a.k = CacheTensor{(const uint8_t *)c.k, c.k_exp, c.k_stride[0] * eb, c.k_stride[1] * eb, (uint32_t)(c.k_stride[2] * eb)};
   a.v = CacheTensor{(const uint8_t *)c.v, c.v_exp, c.v_stride[0] * eb, c.v_stride[1] * eb, (uint32_t)(c.v_stride[2] * eb)};
   a.s = cache_seqs(c, T, cu_q);

@@ -46,7 +46,7 @@ struct AttnCall {
   float scale_log2e;
   int4 *items;  // (divided keys) of each tile of a key head: number of its first part, parts, distance of their numbers
   float *part;
-  int target;   // (divided keys, few rows) parts to aim at
+  unsigned long long *flags, mark;  // (divided keys, few rows) of the parts; what a set flag holds in this call
 };
 
 // One sequence as a kernel sees it.
@@ -69,7 +69,8 @@ __device__ __forceinline__ Seq seq_of(const AttnCall &c, int b) {
 __device__ __forceinline__ void seen_by(const AttnCall &c, const Seq &s, int p, int &lo, int &hi) {
   hi = s.len;
   if (c.causal) {
-    const uint32_t end = (uint32_t)max(p, 0) / (uint32_t)c.causal * (uint32_t)c.causal + (uint32_t)c.causal;  // < 2^32
+    uint32_t end = (uint32_t)max(p, 0) + 1u;
+    if (c.causal > 1) end = (end - 1u) / (uint32_t)c.causal * (uint32_t)c.causal + (uint32_t)c.causal;  // < 2^32
     hi = p < 0 ? 0 : (int)min(end, (uint32_t)s.len);
   }
   lo = c.window ? max(0, hi - c.window) : 0;
@@ -125,6 +126,26 @@ __device__ __forceinline__ Row row_of(const AttnCall &c, const Seq &s, int h, in
   const int i = (int)((unsigned)r / (unsigned)c.G);
   return Row{s.first + i, h * c.G + r - i * c.G};
 }
+
+// The same for the rows of a tile that starts at row r0, by their number in it: i / G for i up to G + tile by a product with
+// 1 / G, which is off by less than one.
+struct Rows {
+  int first, i0, rest, G;
+  float inv;
+  __device__ __forceinline__ Rows(const AttnCall &c, const Seq &s, int r0)
+      : first(s.first), i0((int)((unsigned)r0 / (unsigned)c.G)), rest(r0 - i0 * c.G), G(c.G), inv(1.f / (float)c.G) {}
+  __device__ __forceinline__ int token(int r) const {  // of the sequence's new tokens
+    const int x = rest + r;
+    int q = (int)((float)x * inv);
+    q += (q + 1) * G <= x ? 1 : 0;
+    q -= q * G > x ? 1 : 0;
+    return i0 + q;
+  }
+  __device__ __forceinline__ Row row(int h, int r) const {
+    const int q = token(r);
+    return Row{first + q, h * G + rest + r - (q - i0) * G};
+  }
+};
 
 // What a workgroup works on.
 struct Work {

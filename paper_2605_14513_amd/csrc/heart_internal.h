@@ -299,6 +299,9 @@ inline size_t attn_balanced_bytes(long long BH, long long Nb, int D, int block, 
 // (HEART_ATTN_STATIC_PLAN_BYTES bytes).
 int attn_static_plan(int **ptr);
 
+// A number that no other call of the process has (block_sparse_attn.hip; the low 16 bits are zero).
+unsigned long long call_mark();
+
 int launch_antidiag(const heart_shape &s, const void *q, const void *k, int stride,
                     const unsigned char *refresh, float *scores, float *workspace, hipStream_t st);
 size_t antidiag_workspace_bytes(const heart_shape &s, int stride);
