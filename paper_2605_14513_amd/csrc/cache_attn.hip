@@ -32,6 +32,7 @@ constexpr int kTile = 128;      // rows of a workgroup
 constexpr int kStage = 64;      // keys of a stage
 constexpr int kPlaces = 512;    // places for workgroups: two a CU
 constexpr int kMinStages = 4;   // fewest stages of a part
+constexpr int kPartCost = 8;    // what a part costs beside its stages (launch, first loads, 64 KB written and read), in stages
 
 // floats of one wavefront's part: accumulators, reference exponent and row sum of every lane
 template <int D>
@@ -39,7 +40,8 @@ constexpr int kPartFloats = 64 * (D / 2) + 128;
 
 // (divided keys) The part of workgroup w: the sequences' parts one after the other; of a sequence, head after head, parts,
 // tiles, so that workgroups that read the same keys are neighbours.  Parts have at most L stages, the least L with which
-// there are no more parts than places: found from the lengths by every wavefront on its own.
+// there are no more parts than places, or than twice the places where that ends sooner (300 tiles of one length: two rounds
+// of thirds, not one round of wholes in 300 of 512 places): found from the lengths by every wavefront on its own.
 __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_slot, int lane, Work &k) {
   constexpr int NB = kSplitSeqs / 64;
   int wgs[NB], st[NB];  // tiles of all heads, stages of a tile
@@ -64,11 +66,19 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
       if (j * 64 < c.s.B) n += wgs[j] * (int)((unsigned)(st[j] + L - 1) / (unsigned)L);
     return __builtin_amdgcn_readfirstlane(wave_sum_i32(n));
   };
-  int lo = min(kMinStages, most), hi = most;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (count(mid) <= kPlaces) hi = mid;
-    else lo = mid + 1;
+  auto least = [&](int hi, int places) -> int {
+    int lo = min(kMinStages, hi);
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (count(mid) <= places) hi = mid;
+      else lo = mid + 1;
+    }
+    return lo;
+  };
+  int lo = least(most, kPlaces);
+  if (c.rounds > 1 && lo > kPartCost) {
+    const int two = least(lo, 2 * kPlaces);
+    if (2 * two + kPartCost < lo) lo = two;
   }
   // XCD x has the x-th eighth of the parts
   const int total = count(lo), w = w_xcd * total / kNumXcd + w_slot;
@@ -96,7 +106,24 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
   return true;
 }
 
-template <int D, bool kCodes, bool kSplit>
+// kWhole: a workgroup per tile.  kParts: find_part.  kTail: the tiles of a last round that would not fill the places are
+// divided, c.tail parts each.
+enum CacheMode { kWhole, kParts, kTail };
+// Tile and key head of item i, of n_items = tiles H.  Where there are eight heads or a multiple, an XCD (workgroups are dealt to
+// them in turn) has every eighth head, one after the other, so that its workgroups find each other's keys in its L2 (40 heads
+// of 32760 keys in e4m3: 3000 to 3090 us, 3100 to 3130 with all heads at once).
+__device__ __forceinline__ void item_at(const AttnCall &c, int i, int n_items, int &tile, int &h) {
+  if (c.H % kNumXcd == 0) {
+    const int n = (int)((unsigned)n_items / (unsigned)c.H), s = i / kNumXcd;
+    h = s / n * kNumXcd + i % kNumXcd;
+    tile = s % n;
+  } else {
+    tile = (int)((unsigned)i / (unsigned)c.H);
+    h = i - tile * c.H;
+  }
+}
+
+template <int D, bool kCodes, CacheMode kMode>
 __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   constexpr int DT = D / 32;             // 32-wide d tiles of the output
   constexpr int KS = D / 16;             // k-steps of the first product
@@ -125,20 +152,35 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 
   // ---- what to work on ---------------------------------------------------------------------
   Work wk{0, 0, 0, 0, 1, 1, 0};
-  if constexpr (kSplit) {
+  constexpr bool kSplit = kMode != kWhole;
+  int rec = 0;  // (divided keys) where to note the tile's parts
+  if constexpr (kMode == kParts) {
     if (!find_part(c, (int)(blockIdx.x % kNumXcd), (int)(blockIdx.x / kNumXcd), lane, wk)) return;
   } else {
-    const int tile = (int)(blockIdx.x / (unsigned)c.H);
-    wk.h = (int)(blockIdx.x % (unsigned)c.H);
+    int i = (int)blockIdx.x, tile;
+    if constexpr (kMode == kTail) {
+      // (of the divided tiles: part after part, so that workgroups that read the same keys are neighbours)
+      const int n_tail = c.n_items - c.whole, j = i - c.whole;
+      if (j >= 0) {
+        wk.part = j / n_tail;
+        rec = j - wk.part * n_tail;
+        i = c.whole + rec;
+        wk.parts = c.tail;
+        wk.step = n_tail;
+        wk.slot = j;
+      }
+    }
+    item_at(c, i, c.n_items, tile, wk.h);
     wk.b = seq_of_tile<kTile>(c, tile, lane);
     wk.m = tile - tile_start<kTile>(c, wk.b);
   }
   wk.b = __builtin_amdgcn_readfirstlane(wk.b);
+  wk.m = __builtin_amdgcn_readfirstlane(wk.m);
   const Seq s = seq_of(c, wk.b);
   const int tiles = tiles_of<kTile>(c, s);
-  if (!kSplit) wk.m = __builtin_amdgcn_readfirstlane(wk.m);
   if (wk.m < 0 || wk.m >= tiles) return;
-  if (!kSplit) wk.m = tiles - 1 - wk.m;  // (later tiles see more keys: first)
+  if constexpr (kMode == kParts) rec = (tile_start<kTile>(c, wk.b) + wk.m) * c.H + wk.h;
+  else wk.m = tiles - 1 - wk.m;  // (later tiles see more keys: first)
   const int rows = s.n * c.G, r0 = wk.m * kTile;
   int lo, hi, first_key, end_key, ignore;
   seen_by(c, s, s.pos0 + r0 / c.G, first_key, ignore);
@@ -146,10 +188,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   int stage0 = first_key / kStage, n_stage = max((end_key + kStage - 1) / kStage - stage0, 0);
   int parts = 1;
   if constexpr (kSplit) {
-    const int per = max((n_stage + wk.parts - 1) / wk.parts, 1);
+    const int per = max((n_stage + wk.parts - 1) / wk.parts, kMode == kTail ? 2 * kPartCost : 1);
     parts = max((n_stage + per - 1) / per, 1);
-    if (wk.part == 0 && t == 0)
-      c.items[(long long)(tile_start<kTile>(c, wk.b) + wk.m) * c.H + wk.h] = int4{wk.slot, parts, wk.step, 0};
+    if (wk.part == 0 && t == 0 && (kMode == kParts || wk.parts > 1)) c.items[rec] = int4{wk.slot, parts, wk.step, 0};
     if (wk.part >= parts) return;
     stage0 += wk.part * per;
     n_stage = min(per, n_stage - wk.part * per);
@@ -167,7 +208,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   if (row >= rows) lo = 0, hi = end_key;
   hi = min(hi, end_key);
   // slices from all_lo on and before all_hi need no mask
-  const int all_lo = (int)wave_max_u32((uint32_t)lo), all_hi = (int)wave_min_u32((uint32_t)hi);
+  const int all_lo = __builtin_amdgcn_readfirstlane((int)wave_max_u32((uint32_t)lo));
+  const int all_hi = __builtin_amdgcn_readfirstlane((int)wave_min_u32((uint32_t)hi));
 
   // ---- per-lane constants of the LDS layout ---------------------------------------------
   // Chunk c (16 bytes) of stage row r is stored at chunk position c ^ f(r):
@@ -578,16 +620,22 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 
 // Adds up the parts of the tiles whose keys were divided: a wavefront for 32 rows and 32 columns, lanes as above.
 // Bound by latency (the parts come from the L2s and the memory-side cache): four parts at a time.
-template <int D>
+template <int D, CacheMode kMode>
 __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall c) {
   constexpr float ninf = -__builtin_inff();
   const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
   const int wave = (int)(blockIdx.x % 4), item = (int)(blockIdx.x / 4);
-  const int tile = item / c.H, h = item % c.H;
-  const int b = seq_of_tile<kTile>(c, tile, lane), m = __builtin_amdgcn_readfirstlane(tile - tile_start<kTile>(c, b));
+  int tile, h;
+  if constexpr (kMode == kTail) item_at(c, c.whole + item, c.n_items, tile, h);
+  else tile = item / c.H, h = item % c.H;
+  const int b = seq_of_tile<kTile>(c, tile, lane);
+  int m = __builtin_amdgcn_readfirstlane(tile - tile_start<kTile>(c, b));
   const Seq s = seq_of(c, b);
+  const int tiles = tiles_of<kTile>(c, s);
+  if (m < 0 || m >= tiles) return;
+  if constexpr (kMode == kTail) m = tiles - 1 - m;
   const int rows = s.n * c.G, row = m * kTile + wave * 32 + l32;
-  if (m < 0 || m >= tiles_of<kTile>(c, s) || m * kTile + wave * 32 >= rows) return;
+  if (m * kTile + wave * 32 >= rows) return;
   const int4 it = c.items[item];
   if (it.y <= 1) return;
   float ref = ninf, l = 0.f;
@@ -643,23 +691,46 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
   }
 }
 
-// Divided keys pay where there are fewer tiles than places.
-static bool divides(int B, int H, int T, int Hq) { return B <= kSplitSeqs && most_items(kTile, B, H, T, Hq) < kPlaces; }
+// How the keys of a call of n_items tiles are divided: a function of that number alone.
+struct Division {
+  CacheMode mode;
+  int rounds;       // (kParts) of workgroups at most
+  int whole, tail;  // (kTail) tiles that are not divided, parts of each other
+  long long slots() const { return mode == kParts ? (long long)rounds * kPlaces : mode == kTail ? slots_tail : 0; }
+  long long slots_tail;
+};
+// Fewer tiles than places: all are divided, but of one sequence only where that gives three parts in two rounds.  Up to
+// kTailRounds rounds: the r tiles of the last one, into as many parts (8 at most, 1024 in all) as let it end soonest, a part
+// costing 0.03 of a whole tile beside its keys.  us whole -> divided, 4680 queries, 32760 keys: 4 heads of 37 tiles 534 -> 330, 8
+// (296 tiles) 763 -> 637, 14 (518) 1375 -> 1010, 16 (592) 1389 -> 1169, 18 1445 -> 1320, 32 2352 -> 2252; 9360 keys, 16 heads, 334 -> 300.
+constexpr int kTailRounds = 8, kBrief = 80 * kStage;
+static Division divide(int B, long long n_items) {
+  if (n_items < kPlaces && B <= kSplitSeqs && (B > 1 || 3 * n_items <= 2 * kPlaces))
+    return {kParts, 3 * n_items > kPlaces ? 2 : 1, 0, 1, 0};
+  const int r = (int)(n_items % kPlaces);
+  if (n_items < kPlaces || n_items > kTailRounds * kPlaces || r == 0) return {kWhole, 1, 0, 1, 0};
+  int best = 1;
+  float least = 1e9f;
+  for (int p = 1; p <= 8 && r * p <= 2 * kPlaces; ++p) {
+    const float cost = (float)((r * p + kPlaces - 1) / kPlaces) / p + (p > 1 ? 0.03f * p * r / kPlaces + 0.02f : 0.f);
+    if (cost < least) least = cost, best = p;
+  }
+  if (best == 1) return {kWhole, 1, 0, 1, 0};
+  return {kTail, 1, (int)n_items - r, best, (long long)r * best};
+}
 
 size_t cache_attn_workspace_bytes(int B, int H, int D, int T, int Hq) {
   if (cache_attn_few(B, H, T, Hq)) return cache_attn_few_workspace_bytes(B, H, D, T, Hq);
-  if (!divides(B, H, T, Hq)) return 0;
+  const Division d = divide(B, most_items(kTile, B, H, T, Hq));
   const size_t part = D == 128 ? kPartFloats<128> : kPartFloats<64>;
-  return kPlaces * (sizeof(int4) + 4 * part * sizeof(float));
+  return d.mode == kWhole ? 0 : kPlaces * sizeof(int4) + (size_t)d.slots() * 4 * part * sizeof(float);
 }
 
 template <int D, bool kCodes>
-static int launch_t(const AttnCall &c, bool split, long long items, hipStream_t st) {
+static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
-  constexpr int lds = 4 * kStage * D * 2;  // >= kTile * (D + 8) * 2 of the output staging
-  static_assert(lds >= kTile * (D + 8) * 2 || D == 64, "output staging");
-  constexpr int bytes = lds > kTile * (D + 8) * 2 ? lds : kTile * (D + 8) * 2;
+  constexpr int lds = 4 * kStage * D * 2, staging = kTile * (D + 8) * 2, bytes = lds > staging ? lds : staging;
   auto run = [&](auto kern, long long grid) -> int {
     static DeviceFlags attr_set;
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
@@ -667,9 +738,14 @@ static int launch_t(const AttnCall &c, bool split, long long items, hipStream_t 
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, st, c);
     return check_launch("cache_attn_kernel");
   };
-  if (!split) return run(cache_attn_kernel<D, kCodes, false>, items);
-  if (int rc = run(cache_attn_kernel<D, kCodes, true>, kPlaces)) return rc;
-  hipLaunchKernelGGL((cache_attn_merge_kernel<D>), dim3((unsigned)(items * 4)), dim3(D * 2), 0, st, c);
+  if (d.mode == kWhole) return run(cache_attn_kernel<D, kCodes, kWhole>, c.n_items);
+  if (d.mode == kParts) {
+    if (int rc = run(cache_attn_kernel<D, kCodes, kParts>, d.slots())) return rc;
+    hipLaunchKernelGGL((cache_attn_merge_kernel<D, kParts>), dim3((unsigned)(c.n_items * 4)), dim3(D * 2), 0, st, c);
+  } else {
+    if (int rc = run(cache_attn_kernel<D, kCodes, kTail>, c.whole + d.slots())) return rc;
+    hipLaunchKernelGGL((cache_attn_merge_kernel<D, kTail>), dim3((unsigned)((c.n_items - c.whole) * 4)), dim3(D * 2), 0, st, c);
+  }
   return check_launch("cache_attn_merge_kernel");
 }
 
@@ -689,13 +765,21 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   a.H = c.H, a.G = Hq / c.H, a.causal = causal, a.window = window;
   a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.D)) * 1.4426950408889634f;
   if (cache_attn_few(c.B, c.H, T, Hq)) return launch_cache_attn_few(c, T, Hq, a, workspace, st);
-  const bool split = workspace && divides(c.B, c.H, T, Hq);
-  a.items = (int4 *)workspace;
-  a.part = split ? (float *)(a.items + kPlaces) : nullptr;
   const long long items = most_items(kTile, c.B, c.H, T, Hq);
   if (items > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
-  if (c.D == 128) return codes ? launch_t<128, true>(a, split, items, st) : launch_t<128, false>(a, split, items, st);
-  return codes ? launch_t<64, true>(a, split, items, st) : launch_t<64, false>(a, split, items, st);
+  Division d = divide(c.B, items);
+  // (sequences so short that a second round of parts, and the launch that adds them up, gain nothing: causal attention of 4680 tokens
+  // to themselves, 8 heads 87 us whole, 93 divided, 16 heads 124, 129)
+  const bool brief = a.s.cap <= kBrief && (d.mode == kTail || d.rounds > 1);
+  if (!workspace || brief) d = {kWhole, 1, 0, 1, 0};
+  a.n_items = (int)items;
+  a.rounds = d.rounds;
+  a.whole = d.whole;
+  a.tail = d.tail;
+  a.items = (int4 *)workspace;
+  a.part = workspace ? (float *)(a.items + kPlaces) : nullptr;
+  if (c.D == 128) return codes ? launch_t<128, true>(a, d, st) : launch_t<128, false>(a, d, st);
+  return codes ? launch_t<64, true>(a, d, st) : launch_t<64, false>(a, d, st);
 }
 
 }  // namespace heart

@@ -46,6 +46,7 @@ struct AttnCall {
   float scale_log2e;
   int4 *items;  // (divided keys) of each tile of a key head: number of its first part, parts, distance of their numbers
   float *part;
+  int n_items, rounds, whole, tail;  // tiles of all heads; how their keys are divided (struct Division)
   unsigned long long *flags, mark;  // (divided keys, few rows) of the parts; what a set flag holds in this call
 };
 

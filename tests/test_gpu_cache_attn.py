@@ -163,3 +163,16 @@ def test_no_tokens():
     cache = Cache([50], 2, 128, 32, seed=4)
     q = torch.empty((0, 4, 128), dtype=torch.bfloat16, device="cuda")
     assert heart.heart_cache_attn(q, *cache.args()).shape == (0, 4, 128)
+
+
+@pytest.mark.parametrize("kind,D", [("bf16", 128), ("e4m3", 64)])
+@pytest.mark.parametrize("H,n,kv,causal", [
+    (40, 1664, 2000, 1), (40, 1664, 1700, 0),      # a last round of few tiles: those are divided
+    (43, 1500, 1555, 300),                         # (heads that no XCD has alone)
+    (20, 1900, 2100, 0), (9, 3000, 3100, 0)])      # fewer tiles than places: parts in two rounds, in one
+def test_many_tiles_with_divided_keys(kind, D, H, n, kv, causal):
+    cache = Cache([kv], H, D, 64, kind, seed=H)
+    a, la = run(cache, H, [n], causal=causal, workspace="garbage", what="divided")
+    b, lb = run(cache, H, [n], causal=causal, workspace=None, what="whole")
+    c, lc = run(cache, H, [n], causal=causal, workspace="garbage", what="again")
+    assert torch.equal(a, c) and torch.equal(la, lc)
