@@ -14,7 +14,7 @@
  *     environment variable; an entry point that needs scratch memory takes it as a
  *     workspace argument.  Workspace sizes: heart_workspace_bytes (the hot path),
  *     heart_pool_drift_workspace_bytes, heart_scores_antidiag_workspace_bytes,
- *     heart_ebc_workspace_bytes.
+ *     heart_cache_attn_workspace_bytes, heart_ebc_workspace_bytes.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  A call
  *     only enqueues kernels on that stream and returns; it never synchronises.
  *   - Return value: HEART_OK (0) or a negative error code.  After an error
@@ -323,11 +323,11 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
  * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
  * call's tensors (NULL: each has T/B of them), and the last of them is at position kv_len[b]-1.  Tokens behind cu_q[B], and
- * output rows of them, are left alone.
- * Nothing that these arrays hold leaves the tensors: a position below 0 or from max_pages * page on, and a page outside
- * [0, n_pages), is not written and reads as zeros.  Sequences may share pages that no call writes; of two new tokens
- * at one place of the cache, either or a mixture is kept.
- * T = 0 and N = 0 are valid and launch nothing.
+ * output rows of them, are left alone.  cu_q must not fall and lie in [0, T]; else tokens may be left out.
+ * Nothing that these arrays hold leaves the tensors: a position below 0 or from max_pages * page on is neither written nor
+ * read nor seen, and a page outside [0, n_pages) is not written and reads as zeros.  Sequences may share pages that no call
+ * writes; of two new tokens at one place of the cache, either or a mixture is kept.
+ * T = 0 and N = 0 are valid and launch nothing; T <= 2^30.
  */
 #define HEART_CACHE_BF16 0
 #define HEART_CACHE_E4M3 1
@@ -367,7 +367,8 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * log-sum-exp of the scaled logits.  A query without keys gives zeros (lse = -inf).
  * Precision as heart_block_sparse_attn: bf16 products, fp32 sums, logits scaled and exponentiated in fp32, weights rounded
  * to bf16 for the second contraction (the row sum adds them unrounded).  Cached rows of 8 bits enter as the bf16 values
- * they stand for.  Rows from kv_len on may hold anything.
+ * they stand for.  Rows from kv_len on may hold anything, pages of nobody too; a NaN or an infinity among the first kv_len
+ * tokens may also reach queries that do not see it.  out must not overlap q.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
  * B, H, D alone), or NULL.  With it the keys of few queries are divided over the chip, into parts that depend on all
  * lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on

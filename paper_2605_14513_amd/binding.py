@@ -481,7 +481,8 @@ def heart_cache_attn_workspace_bytes(q, k_cache, page_table) -> int:
 def heart_cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None, causal: int = 1,
                      window: int = 0, scale: float = 0.0, out=None, lse=None, workspace="auto"):
     """Attention of the new tokens' queries (bf16 [T,Hq,D]) over the cache, which holds their keys and values already (the
-    cache's arguments: heart_cache_write); returns bf16 out like q.
+    cache's arguments: heart_cache_write); returns bf16 out like q (rows behind cu_q[B] are left as they are in a given out,
+    and hold anything in a new one).
 
     causal: 0 a query sees the whole sequence, n > 0 the blocks of n positions up to its own; window: only the last so
     many of these keys (0: all).  lse: fp32 [Hq,T] or None.  workspace: a GPU tensor of at least

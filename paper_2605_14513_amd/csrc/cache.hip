@@ -6,6 +6,10 @@
 // anywhere, so in writing each of the first 16 lanes finds the place of one token and the others take it from there; the
 // rows themselves are loaded meanwhile.  A row of D elements is held by D/8 neighbouring lanes: the maximum over a row is
 // three or four lane exchanges on the VALU.
+//
+// us: reading 32760 tokens of 12 heads of 128 from e4m3 (303 MB in and out) 60 (5.1 TB/s, a copy of 512 MB 4.7), of 40 heads 189;
+// writing 4680 tokens of 40 heads and reading them back 62; the tokens of 64 sequences 4.5.  Stores past the caches make the
+// first 53, but the pooling that reads what was read back then takes 36 instead of 23.
 #include "cache_device.h"
 
 namespace heart {

@@ -399,6 +399,7 @@ int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, con
   if (T == 0) return HEART_OK;
   if (!q || !out) return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
   if (!aligned16(q) || !aligned16(out)) return fail(HEART_EUNSUPPORTED, "%s: q and out must be 16-byte aligned", fn);
+  if (q == out) return fail(HEART_EINVAL, "%s: out must not be q", fn);
   if (!chunk_strides_ok(q_stride, 2) || !chunk_strides_ok(o_stride, 2))
     return fail(HEART_EUNSUPPORTED, "%s: strides must be multiples of 8 elements", fn);
   if ((long long)T * Hq > 0x3fffffffLL || ((long long)T + cache->B) * Hq > 0x7fffffffLL)

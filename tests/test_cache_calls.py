@@ -37,12 +37,12 @@ def strides(*s):
     return (ctypes.c_longlong * len(s))(*s)
 
 
-def calls(lib, c, T=3, q=F, qs=(512, 128), cu=None, Hq=4, causal=1, window=0, ws=None, ws_bytes=0, N=5, rs=(1024, 512, 128)):
+def calls(lib, c, T=3, q=F, out=2 * F, qs=(512, 128), cu=None, Hq=4, causal=1, window=0, ws=None, ws_bytes=0, N=5, rs=(1024, 512, 128)):
     r = None if c is None else ctypes.byref(c)
     s2, s3 = (strides(*qs) if qs else None), (strides(*rs) if rs else None)
     return {"write": lambda: lib.heart_cache_write(r, T, q, s2, q, s2, cu, None),
             "read": lambda: lib.heart_cache_read(r, N, q, s3, q, s3, None),
-            "attn": lambda: lib.heart_cache_attn(r, T, Hq, q, s2, cu, causal, window, 0.0, q, s2, None, ws, ws_bytes, None)}
+            "attn": lambda: lib.heart_cache_attn(r, T, Hq, q, s2, cu, causal, window, 0.0, q if q != F else out, s2, None, ws, ws_bytes, None)}
 
 
 def test_struct_layout_matches_the_header(lib):
@@ -87,7 +87,7 @@ def test_no_cache(lib):
     ("write attn", dict(qs=(512, 100)), EUNSUPPORTED), ("write attn", dict(qs=(516, 128)), EUNSUPPORTED),
     ("write attn", dict(qs=None), EINVAL), ("read", dict(rs=None), EINVAL), ("read", dict(rs=(1024, 512, 4)), EUNSUPPORTED),
     ("attn", dict(Hq=0), EINVAL), ("attn", dict(Hq=3), EINVAL), ("attn", dict(Hq=-2), EINVAL), ("attn", dict(causal=-1), EINVAL),
-    ("attn", dict(window=-1), EINVAL), ("attn", dict(T=3 * 2**28, Hq=4), EUNSUPPORTED), ("write", dict(T=3 * 2**29), EUNSUPPORTED),
+    ("attn", dict(window=-1), EINVAL), ("attn", dict(out=F), EINVAL), ("attn", dict(T=3 * 2**28, Hq=4), EUNSUPPORTED), ("write", dict(T=3 * 2**29), EUNSUPPORTED),
     ("attn", dict(ws=F + 8, ws_bytes=1 << 40), EUNSUPPORTED), ("attn", dict(ws=F, ws_bytes=100), EINVAL)])
 def test_arguments_that_a_call_refuses(lib, which, change, code):
     for name in which.split():
