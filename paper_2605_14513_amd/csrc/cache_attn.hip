@@ -306,25 +306,22 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
       raw_exp[is_v][ii] = __builtin_amdgcn_raw_buffer_load_b8(es, (uint32_t)r, 0, 0);
     }
   };
-  auto store_codes = [&](int is_v, int ii, int buf) __attribute__((always_inline)) {
+  auto store_codes = [&](int is_v, int ii, int p, int buf) __attribute__((always_inline)) {
     const int r = wave * 16 + ii * RPC + crow, f = swizzle(is_v, r);
     unsigned char *dst = smem + (2 * is_v + buf) * TILE_B + r * ROWB;
     const u32x4_t x = raw[is_v][ii];
     const float unit = unit_of(raw_exp[is_v][ii]);
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const u32x4_t y = {codes_to_bf16<false>(x[2 * p], unit), codes_to_bf16<true>(x[2 * p], unit),
-                         codes_to_bf16<false>(x[2 * p + 1], unit), codes_to_bf16<true>(x[2 * p + 1], unit)};
-      *reinterpret_cast<u32x4_t *>(dst + (((2 * cchunk + p) ^ f) * 16)) = y;
-    }
+    const u32x4_t y = {codes_to_bf16<false>(x[2 * p], unit), codes_to_bf16<true>(x[2 * p], unit),
+                       codes_to_bf16<false>(x[2 * p + 1], unit), codes_to_bf16<true>(x[2 * p + 1], unit)};
+    *reinterpret_cast<u32x4_t *>(dst + (((2 * cchunk + p) ^ f) * 16)) = y;
   };
   // step j of KS of bringing stage i to buffer `buf`; (codes) stage i is in registers, stage i + 1 is loaded behind it
   auto bring = [&](int j, int i, int buf) __attribute__((always_inline)) {
     if constexpr (kCodes) {
 #pragma unroll
-      for (int ii = 0; ii < 2 * CPW; ++ii)
-        if (ii * (KS - 2) / (2 * CPW) == j) store_codes(ii / CPW, ii % CPW, buf);
-      if (j == KS - 2) load_codes(0, i + 1);
+      for (int hh = 0; hh < 4 * CPW; ++hh)
+        if (hh * KS / (4 * CPW) == j) store_codes(hh / (2 * CPW), hh / 2 % CPW, hh % 2, buf);
+      if (j == KS / 2 - 1) load_codes(0, i + 1);
       if (j == KS - 1) load_codes(1, i + 1);
     } else {
 #pragma unroll
