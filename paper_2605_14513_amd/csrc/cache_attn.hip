@@ -16,8 +16,8 @@
 //
 // Stages.  K stage i holds slices 2i, 2i + 1; V stage i slices 2i - 1, 2i, so that one barrier per 64 keys retires both. Each
 // of the four wavefronts brings 16 rows of a stage, and pages hold a multiple of 16 tokens, so a wavefront needs one
-// page for a stage: a buffer descriptor over the rows that are there (rows from kv_len on, and pages that the table does
-// not name, are out of its range and arrive as zeros).  The page ids of 64 stages lie in one register, a lane each.
+// page for a stage: a buffer descriptor over the rows that are there (rows that no query of the tile sees, from kv_len on
+// in any case, and pages that the table does not name, are out of its range and arrive as zeros).  The page ids of 64 stages lie in one register, a lane each.
 //   bf16: LDS-direct loads, double-buffered, two slices ahead.
 //   e4m3: the codes are loaded into registers a stage earlier still and written to LDS as the bf16 values that they
 //     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
@@ -185,6 +185,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   int lo, hi, first_key, end_key, ignore;
   seen_by(c, s, s.pos0 + r0 / c.G, first_key, ignore);
   seen_by(c, s, s.pos0 + min(r0 + kTile - 1, rows - 1) / c.G, ignore, end_key);
+  const int tile_end = __builtin_amdgcn_readfirstlane(end_key);  // keys from here on no row of the tile sees: zeros
   int stage0 = first_key / kStage, n_stage = max((end_key + kStage - 1) / kStage - stage0, 0);
   int parts = 1;
   if constexpr (kSplit) {
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     for (int is_v = 0; is_v < 2; ++is_v) {
       const int key = key0 + (base + lane) * kStage - 32 * is_v + 16 * wave;
       ids[is_v] = -1;
-      if (base + lane <= n_stage && key >= 0 && key < s.len) ids[is_v] = cache_page(c.s, wk.b, key);
+      if (base + lane <= n_stage && key >= 0 && key < tile_end) ids[is_v] = cache_page(c.s, wk.b, key);
     }
   };
   const int in_page = (1 << c.s.page_shift) - 1;
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     const int off = key & in_page;
     addr = (uint64_t)(x.p + max(id, 0) * x.page + wk.h * x.head + off * (long long)x.row);
     if constexpr (kCodes) exp_addr = (uint64_t)(x.exp + ((((long long)max(id, 0) * c.H + wk.h) << c.s.page_shift) + off));
-    return id < 0 ? 0 : min(s.len - key, 16);
+    return id < 0 ? 0 : min(tile_end - key, 16);
   };
   // LDS-direct loads (bf16): one instruction moves 16 bytes per lane to 1 KB of consecutive LDS; lane l lands at chunk
   // position l % CPR of row l / CPR and therefore fetches chunk (l % CPR) ^ f(row).

@@ -1,6 +1,6 @@
 // heart_cache_attn where a key head has few rows (single tokens, drafts of a few): bound by reading the cache.
 //
-// A tile is 16 or 32 rows, and a workgroup's four wavefronts divide the keys of its part among them, slice by slice, each
+// A tile is 16 rows, and a workgroup's four wavefronts divide the keys of its part among them, slice by slice, each
 // with a softmax state of its own that is put together at the end.  Every wavefront brings its own slices into its own
 // part of LDS, so the loop has no barrier, only waits for the wavefront's own loads:
 //   S^T (keys x rows) = K . Q^T,  O^T (d x rows) += V^T . P^T     with v_mfma_f32_16x16x32_bf16 (16x16x16 for slices of 16)
@@ -14,12 +14,11 @@
 // rounded (a power of two rounds nothing).
 //
 // Dividing the keys: struct Shares.  The workgroup that finds all parts of a tile there adds them up.
-#include <type_traits>
-
 #include "cache_attn_device.h"
 
 namespace heart {
 
+constexpr int kFewTile = 16;     // rows of a workgroup
 constexpr int kFewStage = 128;   // keys that shares are measured in
 constexpr int kFewMin = 2;       // shortest share, in stages
 constexpr int kFewCut = 1;       // fewest stages of a part: a cut closer to an end of its tile goes there
@@ -31,8 +30,8 @@ constexpr long long kFewOnce = 80ll << 20;
 constexpr int kFewItems = 8192;   // most tiles of a call whose keys are divided
 constexpr int kFewPlaces = 512;   // shares at most: places for workgroups, two a CU
 
-template <int D, int NR>
-constexpr int kFewPart = 16 * NR * (D + 2);  // floats of a part: rows of D, references, row sums
+template <int D>
+constexpr int kFewPart = kFewTile * (D + 2);  // floats of a part: rows of D, references, row sums
 
 // How the keys of all tiles (sequences; of each, heads, tiles) are dealt out.  Every wavefront finds its own from the lengths:
 // no plan, no queue, and no workgroup waits for another.
@@ -42,13 +41,14 @@ constexpr int kFewPart = 16 * NR * (D + 2);  // floats of a part: rows of D, ref
 //           stages, and a tile costs COST beside its stages (64 ragged sequences: 81 us with shares; 86 to 95 with parts of
 //           different lengths in two or three rounds of workgroups)
 // (NB: sequences a lane.  One where that is enough: code that is jumped over has to be fetched all the same.)
-template <int TILE, int COST, int NB_>
+template <int COST, int NB_>
 struct Shares {
   static constexpr int NB = NB_;
   Seq s[NB];                           // sequences 64 j + lane:
   int tiles[NB], st[NB], before[NB];   // tiles of a head, stages of each, length of what is before
   int n, step, rest, total;
-  int most;                            // (parts) stages of a part at most, 0 = shares
+  int part_log;                        // (parts) log2 of a part's stages at most, 0 = shares
+  __device__ __forceinline__ int parts_of(int j) const { return (st[j] + (1 << part_log) - 1) >> part_log; }
   __device__ __forceinline__ int cut(int k) const { return k * step + min(k, rest); }
   // the last cut at or before v
   __device__ __forceinline__ int last_cut(int v) const {
@@ -61,7 +61,7 @@ struct Shares {
     return x >= len ? len : x < kFewCut ? 0 : len - x < kFewCut ? len : x;
   }
   // of a divided tile (one with a cut at least kFewCut from either end) at `tile0`: share of its first part, number of parts
-  __device__ __forceinline__ void parts_of(int tile0, int len, int &first, int &parts) const {
+  __device__ __forceinline__ void cut_parts(int tile0, int len, int &first, int &parts) const {
     first = last_cut(tile0 + 2 * kFewCut + COST - 2);
     parts = last_cut(tile0 + 2 * (len - kFewCut) + COST) + 1 - first;
   }
@@ -80,8 +80,8 @@ struct Shares {
         if (b < c.s.B) {
           s[j] = seq_of(c, b);
           falls = falls || (c.s.cu && c.s.cu[b + 1] < c.s.cu[b]);
-          tiles[j] = tiles_of<TILE>(c, s[j]);
-          st[j] = stages_of<TILE, kFewStage>(c, s[j]);
+          tiles[j] = tiles_of<kFewTile>(c, s[j]);
+          st[j] = stages_of<kFewTile, kFewStage>(c, s[j]);
         }
         const int len = tiles[j] * c.H * (2 * st[j] + COST), end = at + wave_scan_i32(len);
         before[j] = end - len;
@@ -90,15 +90,15 @@ struct Shares {
     }
     total = at;
     n = 0;
-    for (most = kFewMin; most <= 4 * kFewMin; most *= 2) {
+    for (part_log = 1; part_log <= 3; ++part_log) {
 #pragma unroll
       for (int j = 0; j < NB; ++j)
-        if (j * 64 < c.s.B) n += tiles[j] * ((st[j] + most - 1) / most);
+        if (j * 64 < c.s.B) n += tiles[j] * parts_of(j);
       n = __builtin_amdgcn_readfirstlane(wave_sum_i32(n)) * c.H;
       if (n <= places) return at > 0 && !__any(falls);
       n = 0;
     }
-    most = 0;
+    part_log = 0;
     n = min(places, max(at / (2 * kFewMin + COST), 1));
     step = (int)((unsigned)at / (unsigned)n);
     rest = at - step * n;
@@ -118,11 +118,11 @@ struct FewShape {
 };
 
 // SEQS: sequences a lane where the keys are divided, 0 = they are not
-template <int D, bool kCodes, int NR, int SEQS>
+template <int D, bool kCodes, int SEQS>
 __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c) {
   using F = FewShape<D, kCodes>;
   constexpr bool kSplit = SEQS > 0;
-  constexpr int TILE = 16 * NR, ROWB = F::ROWB, SK = F::SK, NT = F::NT, NI = F::NI;
+  constexpr int TILE = kFewTile, ROWB = F::ROWB, SK = F::SK, NT = F::NT, NI = F::NI;
   constexpr int NC = ROWB / 16, RPB = 256 / ROWB, RPI = 1024 / ROWB;  // chunks of a row, rows per 256 bytes, rows of a load
   constexpr int KS = D / 32, DT = D / 16;
   constexpr int NLOAD = NT * NI;                       // loads of K (or V) of a slice
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   // ---- what to work on -----------------------------------------------------------------------
   // (shares) the share's number and ends; of the tile: its sequence, number in it, start; of the sequence: tiles of a head and
   // of all, stages of a tile
-  using Sh = Shares<TILE, 512 / ROWB, kSplit ? SEQS : 1>;
+  using Sh = Shares<512 / ROWB, kSplit ? SEQS : 1>;
   [[maybe_unused]] Sh sh;
   int share = 0, cut0 = 0, cut1 = 0, b = 0, number = 0, tile0 = 0, n_head = 1, n_seq = 0, len = 1;
   int first_part = 0, parts = 0;  // (parts, and of a divided tile) number of its first part, their number
@@ -157,12 +157,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
     if (!sh.find(c, (int)gridDim.x, lane)) return;
     share = (int)blockIdx.x;
     if (share >= sh.n) return;
-    if (sh.most) {
+    if (sh.part_log) {
       int at = 0;
 #pragma unroll
       for (int j = 0; j < Sh::NB; ++j)
         if (j * 64 < c.s.B) {
-          const int of_tile = (sh.st[j] + sh.most - 1) / sh.most, all = sh.tiles[j] * c.H * of_tile;
+          const int of_tile = sh.parts_of(j), all = sh.tiles[j] * c.H * of_tile;
           const int end = at + wave_scan_i32(all);
           const unsigned long long here = __ballot(end - all <= share && share < end);
           if (here) {
@@ -192,10 +192,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
     }
   } else {
     const int tile = (int)(blockIdx.x / (unsigned)c.H);
-    b = seq_of_tile<TILE>(c, tile, lane);
+    b = seq_of_tile<kFewTile>(c, tile, lane);
     s = seq_of(c, b);
-    number = __builtin_amdgcn_readfirstlane(tile - tile_start<TILE>(c, b));
-    if (number < 0 || number >= tiles_of<TILE>(c, s)) return;
+    number = __builtin_amdgcn_readfirstlane(tile - tile_start<kFewTile>(c, b));
+    if (number < 0 || number >= tiles_of<kFewTile>(c, s)) return;
   }
   // ---- LDS layout: 16-byte chunk c of slice row r at chunk position c ^ f(r), so that the rows read together fall into
   // different banks
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   for (;;) {
   int x0 = 0, x1 = len;  // stages of the tile that belong to the share; a cut near an end of the tile is at that end
   if constexpr (kSplit) {
-    if (sh.most) {
+    if (sh.part_log) {
       x0 = (share - first_part) * len / parts;
       x1 = (share - first_part + 1) * len / parts;
     } else {
@@ -261,6 +261,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   seen_by(c, s, s.pos0 + at0.token(n_rows - 1), ignore, end_key);
   int stage0 = first_key / kFewStage, n_stage = max((end_key + kFewStage - 1) / kFewStage - stage0, 0);
   const bool partial = kSplit && x1 - x0 < len;
+  const int tile_end = __builtin_amdgcn_readfirstlane(end_key);  // keys from here on no row of the tile sees: zeros
   if (partial) {
     // (of the n_stage stages that this tile has: len is that of the sequence's longest)
     const int y0 = n_stage == len ? x0 : (int)((long long)x0 * n_stage / len);
@@ -273,16 +274,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   end_key = __builtin_amdgcn_readfirstlane(end_key);
   const int n_slice = __builtin_amdgcn_readfirstlane(max((end_key - key0 + 4 * SK - 1) / (4 * SK), 0));
 
-  int lo[NR], hi[NR], all_lo = 0, all_hi = 0x7fffffff;
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int row = 16 * n + l16;
-    seen_by(c, s, s.pos0 + at0.token(min(row, n_rows - 1)), lo[n], hi[n]);
-    if (row >= n_rows) lo[n] = 0, hi[n] = end_key;  // (rows past the end see what is there)
-    hi[n] = min(hi[n], end_key);
-    all_lo = max(all_lo, (int)wave_max_u32((uint32_t)lo[n]));
-    all_hi = min(all_hi, (int)wave_min_u32((uint32_t)hi[n]));
-  }
+  int lo, hi;  // keys that this lane's row sees of the part
+  seen_by(c, s, s.pos0 + at0.token(min(l16, n_rows - 1)), lo, hi);
+  if (l16 >= n_rows) lo = 0, hi = end_key;  // (rows past the end see what is there)
+  hi = min(hi, end_key);
+  // slices from all_lo on and before all_hi need no mask (in vector registers: as scalars they made the loop 7 % slower, 64 ragged
+  // sequences in e4m3 73.6 -> 78.8 us)
+  const int all_lo = (int)wave_max_u32((uint32_t)lo);
+  const int all_hi = (int)wave_min_u32((uint32_t)hi);
 
   // ---- page ids of slices base .. base + 63, lane l that of slice base + l, by tile
   int ids[NT];
@@ -308,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
       const int key = key0 + i * (4 * SK) + 16 * n, off = key & in_page;
       const int id = i < n_slice ? __builtin_amdgcn_readlane(ids[n], i & 63) : -1;
       const uint64_t addr = (uint64_t)(x.p + max(id, 0) * x.page + head * x.head + off * (long long)x.row);
-      const int there = id < 0 ? 0 : min(s.len - key, 16);
+      const int there = id < 0 ? 0 : min(tile_end - key, 16);
       u32x4_t rs;
       rs.x = __builtin_amdgcn_readfirstlane((uint32_t)addr);
       rs.y = __builtin_amdgcn_readfirstlane((uint32_t)(addr >> 32) & 0xffffu);
@@ -356,23 +355,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   };
 
   // ---- state of the rows -----------------------------------------------------------------------
-  Frag8 qf[NR][KS];
-  f32x4_t o[NR][DT];
-  float m_ref[NR], c0[NR], l_run[NR];
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const Row at = at0.row(head, min(16 * n + l16, n_rows - 1));
+  Frag8 qf[KS];
+  f32x4_t o[DT];
+  float m_ref = ninf, c0 = 0.f, l_run = 0.f;  // reference exponent, minus that in raw logits, this lane's part of the row sum
+  {
+    const Row at = at0.row(head, min(l16, n_rows - 1));
     const uint16_t *src = c.q + at.token * c.qt + at.head * c.qh;
     // (codes: a lane's 16 bytes are d 16 (4 i + g) .. of k-steps 2 i and 2 i + 1)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      qf[n][ks].u = *reinterpret_cast<const u32x4_t *>(src + (kCodes ? 16 * (4 * (ks / 2) + g) + 8 * (ks & 1) : 32 * ks + 8 * g));
-    m_ref[n] = ninf;
-    c0[n] = 0.f;
-    l_run[n] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[n][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      qf[ks].u = *reinterpret_cast<const u32x4_t *>(src + (kCodes ? 16 * (4 * (ks / 2) + g) + 8 * (ks & 1) : 32 * ks + 8 * g));
   }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const float scale_log2e = c.scale_log2e, inv_scale = 1.f / scale_log2e;
 
   if (n_slice > 0) {
@@ -415,69 +410,64 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
       if (((i + 2) & 63) == 0) load_ids(i + 2);
       bring(0, i + 2);
       bring_exps(i + 2, 2);
-      f32x4_t x[NR][NT];
+      f32x4_t x[NT];
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
+      for (int n = 0; n < NT; ++n) {
+        f32x4_t acc = {c0, c0, c0, c0};
 #pragma unroll
-        for (int kt = 0; kt < NT; ++kt) {
-          f32x4_t acc = {c0[n], c0[n], c0[n], c0[n]};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kt][ks].v, qf[n][ks].v, acc, 0, 0, 0);
-          x[n][kt] = acc * scale_log2e;
-        }
+        for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][ks].v, qf[ks].v, acc, 0, 0, 0);
+        x[n] = acc * scale_log2e;
+      }
       if (key < all_lo || key + SK > all_hi) {
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int kt = 0; kt < NT; ++kt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = key + 16 * kt + 4 * g + e;
-              if (j < lo[n] || j >= hi[n]) x[n][kt][e] = ninf;
-            }
-      }
-      // ---- the reference moves where a logit exceeds it by more than the slack ------------------
-#pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        float m = ninf;
-#pragma unroll
-        for (int kt = 0; kt < NT; ++kt) m = fmaxf(fmaxf(fmaxf(m, x[n][kt][0]), x[n][kt][1]), fmaxf(x[n][kt][2], x[n][kt][3]));
-        const bool first = m_ref[n] == ninf;
-        if (__any(m > kSlack || (first && m > ninf))) {
-          uint32_t a, b;
-          swap_rows16(__float_as_uint(m), a, b);
-          m = fmaxf(__uint_as_float(a), __uint_as_float(b));
-          swap_halves32(__float_as_uint(m), a, b);
-          m = fmaxf(__uint_as_float(a), __uint_as_float(b));
-          const bool bump = m > kSlack || (first && m > ninf);
-          const float delta = bump ? m : 0.f, m_new = bump ? (first ? 0.f : m_ref[n]) + m : m_ref[n];
-          const float alpha = bump ? __builtin_amdgcn_exp2f(m_ref[n] - m_new) : 1.f;
-          l_run[n] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) o[n][dt] *= alpha;
-#pragma unroll
-          for (int kt = 0; kt < NT; ++kt) x[n][kt] -= delta;
-          m_ref[n] = m_new;
-          c0[n] = m_new == ninf ? 0.f : -m_new * inv_scale;
-        }
-      }
-      // ---- weights ------------------------------------------------------------------------------
-      Frag8 pf[NR][(NT + 1) / 2];
-#pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int kt = 0; kt < NT; ++kt) {
-          float p[4];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(x[n][kt][e]);
-            l_run[n] += p[e];
-            if constexpr (kCodes) p[e] *= vu[kt][e];
+            const int j = key + 16 * n + 4 * g + e;
+            if (j < lo || j >= hi) x[n][e] = ninf;
           }
-          pf[n][kt / 2].u[2 * (kt & 1)] = cvt_pk_bf16(p[0], p[1]);
-          pf[n][kt / 2].u[2 * (kt & 1) + 1] = cvt_pk_bf16(p[2], p[3]);
+      }
+      // ---- the reference moves where a logit exceeds it by more than the slack ------------------
+      float m = ninf;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) m = fmaxf(fmaxf(fmaxf(m, x[n][0]), x[n][1]), fmaxf(x[n][2], x[n][3]));
+      const bool first = m_ref == ninf;
+      if (__any(m > kSlack || (first && m > ninf))) {
+        uint32_t a, b;
+        swap_rows16(__float_as_uint(m), a, b);
+        m = fmaxf(__uint_as_float(a), __uint_as_float(b));
+        swap_halves32(__float_as_uint(m), a, b);
+        m = fmaxf(__uint_as_float(a), __uint_as_float(b));
+        const bool bump = m > kSlack || (first && m > ninf);
+        const float delta = bump ? m : 0.f, m_new = bump ? (first ? 0.f : m_ref) + m : m_ref;
+        const float alpha = bump ? __builtin_amdgcn_exp2f(m_ref - m_new) : 1.f;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) x[n] -= delta;
+        m_ref = m_new;
+        c0 = m_new == ninf ? 0.f : -m_new * inv_scale;
+      }
+      // ---- weights ------------------------------------------------------------------------------
+      // (as a sum of two bf16: the weights of few rows can have 16 bits where reading the cache is what takes the time)
+      Frag8 pf[(NT + 1) / 2], pl[(NT + 1) / 2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(x[n][e]);
+          l_run += p[e];
+          if constexpr (kCodes) p[e] *= vu[n][e];
         }
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const uint32_t w = cvt_pk_bf16(p[e], p[e + 1]);
+          pf[n / 2].u[2 * (n & 1) + e / 2] = w;
+          pl[n / 2].u[2 * (n & 1) + e / 2] = cvt_pk_bf16(p[e] - bf16lo(w), p[e + 1] - bf16hi(w));
+        }
+      }
       // ---- O^T ------------------------------------------------------------------------------------
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER + NLOAD + (kCodes ? 1 : 0)) : "memory");  // V of slice i is there
 #pragma unroll
@@ -498,16 +488,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
               const u32x2_t r2 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 16 * ROWB)));
               a.u = u32x4_t{r.x, r.y, r2.x, r2.y};
             }
-#pragma unroll
-            for (int n = 0; n < NR; ++n) o[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, pf[n][kp].v, o[n][dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, pl[kp].v, o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, pf[kp].v, o[dt], 0, 0, 0);
           }
         } else {
           const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sv + voff[dt]));
-#pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            const u32x2_t b = {pf[n][0].u[0], pf[n][0].u[1]};
-            o[n][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s16x4_t, b), o[n][dt], 0, 0, 0);
-          }
+          const u32x2_t b = {pf[0].u[0], pf[0].u[1]}, b2 = {pl[0].u[0], pl[0].u[1]};
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s16x4_t, b2), o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s16x4_t, b), o[dt], 0, 0, 0);
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -521,22 +509,21 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   // ---- the four wavefronts' states put together ---------------------------------------------------
   float *so = reinterpret_cast<float *>(smem);
   static_assert(TILE * D * 4 <= F::WAVE_B, "a wavefront's output fits its part of LDS");
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
+  {
     uint32_t x, y;
-    swap_rows16(__float_as_uint(l_run[n]), x, y);
+    swap_rows16(__float_as_uint(l_run), x, y);
     float l = __uint_as_float(x) + __uint_as_float(y);
     swap_halves32(__float_as_uint(l), x, y);
     l = __uint_as_float(x) + __uint_as_float(y);
     if (g == 0) {
-      s_ref[wave][16 * n + l16] = m_ref[n];
-      s_sum[wave][16 * n + l16] = l;
+      s_ref[wave][l16] = m_ref;
+      s_sum[wave][l16] = l;
     }
-    // (16-byte chunk c of row r at c ^ (r % 16))
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      *reinterpret_cast<f32x4_t *>(so + (size_t)wave * (F::WAVE_B / 4) + (16 * n + l16) * D + (((4 * dt + g) ^ l16) * 4)) = o[n][dt];
   }
+  // (16-byte chunk c of row r at c ^ (r % 16))
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+    *reinterpret_cast<f32x4_t *>(so + (size_t)wave * (F::WAVE_B / 4) + l16 * D + (((4 * dt + g) ^ l16) * 4)) = o[dt];
   __syncthreads();
   constexpr int CH = D / 8;  // threads of a row, 8 elements each
   auto write_row = [&](int r, int ch, f32x4_t y0, f32x4_t y1, float ref, float l) __attribute__((always_inline)) {
@@ -550,7 +537,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   };
   constexpr int kAgent = 16;  // (sc1: past the L2 of this XCD, where the workgroups of all XCDs meet)
   auto part_rsrc = [&](int slot) __attribute__((always_inline)) -> __amdgpu_buffer_rsrc_t {
-    return __builtin_amdgcn_make_buffer_rsrc(c.part + (size_t)slot * kFewPart<D, NR>, 0, (int)(kFewPart<D, NR> * sizeof(float)), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(c.part + (size_t)slot * kFewPart<D>, 0, (int)(kFewPart<D> * sizeof(float)), 0x00020000);
   };
   for (int i = t; i < n_rows * CH; i += 256) {
     const int r = i / CH, ch = i % CH;
@@ -582,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   }
   if constexpr (kSplit) if (partial) {
     // ---- the parts of a divided tile are added up by the workgroup that finds all of them there --------
-    if (!sh.most) sh.parts_of(tile0, len, first_part, parts);
+    if (!sh.part_log) sh.cut_parts(tile0, len, first_part, parts);
     const int k0 = __builtin_amdgcn_readfirstlane(first_part);
     parts = __builtin_amdgcn_readfirstlane(parts);
     // (a share leaves two parts at most: that of the tile it starts in, and of one that starts in it)
@@ -609,53 +596,50 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
       // rows' parts are dealt out to groups of D/8 threads (few rows have many parts), whose sums meet in LDS
       constexpr int NG = 256 / CH;
       const __amdgpu_buffer_rsrc_t all_parts =
-          __builtin_amdgcn_make_buffer_rsrc(c.part, 0, (int)(2u * gridDim.x * (uint32_t)(kFewPart<D, NR> * sizeof(float))), 0x00020000);
+          __builtin_amdgcn_make_buffer_rsrc(c.part, 0, (int)(2u * gridDim.x * (uint32_t)(kFewPart<D> * sizeof(float))), 0x00020000);
       float(*g_o)[D] = reinterpret_cast<float(*)[D]>(smem);
       float *g_ref = reinterpret_cast<float *>(smem) + NG * D, *g_sum = g_ref + NG;
       const int grp = t / CH, ch = t % CH;
       // groups of a row: as many as there are, MP parts a group at least
       constexpr int MP = 4;
-      const int gp = max(min(NG / n_rows, (parts + MP - 1) / MP), 1), at_once = NG / gp;
-      for (int base = 0; base < n_rows; base += at_once) {
-        const int r = base + grp / gp, p0 = grp % gp;
-        const bool mine = grp < at_once * gp && r < n_rows;
-        float ref = ninf, l = 0.f;
-        f32x4_t y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
-        if (mine)
-          for (int p = p0; p < parts; p += MP * gp) {
-            float ms[MP], ls[MP];
-            f32x4_t u[MP], v[MP];
+      const int gp = max(min(NG / n_rows, (parts + MP - 1) / MP), 1), r = grp / gp, p0 = grp % gp;
+      static_assert(kFewTile <= NG, "a group a row at least");
+      const bool mine = r < n_rows;
+      float ref = ninf, l = 0.f;
+      f32x4_t y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
+      if (mine)
+        for (int p = p0; p < parts; p += MP * gp) {
+          float ms[MP], ls[MP];
+          f32x4_t u[MP], v[MP];
 #pragma unroll
-            for (int i = 0; i < MP; ++i) {
-              const uint32_t at = (uint32_t)slot(min(p + i * gp, parts - 1)) * (uint32_t)(kFewPart<D, NR> * sizeof(float));
-              ms[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(all_parts, at + (uint32_t)(TILE * D + r) * 4u, 0, kAgent));
-              ls[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(all_parts, at + (uint32_t)(TILE * D + TILE + r) * 4u, 0, kAgent));
-              u[i] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(all_parts, at + (uint32_t)(r * D + 8 * ch) * 4u, 0, kAgent));
-              v[i] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(all_parts, at + (uint32_t)(r * D + 8 * ch + 4) * 4u, 0, kAgent));
-            }
-            const float old = ref;
-#pragma unroll
-            for (int i = 0; i < MP; ++i)
-              if (p + i * gp < parts) ref = fmaxf(ref, ms[i]);
-            const float fin = ref == ninf ? 0.f : ref;
-            const float alpha = __builtin_amdgcn_exp2f(old - fin);
-            l *= alpha;
-            y0 *= alpha;
-            y1 *= alpha;
-#pragma unroll
-            for (int i = 0; i < MP; ++i) {
-              if (p + i * gp >= parts) continue;
-              const float w = __builtin_amdgcn_exp2f(ms[i] - fin);
-              l = fmaf(ls[i], w, l);
-              y0 += u[i] * w;
-              y1 += v[i] * w;
-            }
+          for (int i = 0; i < MP; ++i) {
+            const uint32_t at = (uint32_t)slot(min(p + i * gp, parts - 1)) * (uint32_t)(kFewPart<D> * sizeof(float));
+            ms[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(all_parts, at + (uint32_t)(TILE * D + r) * 4u, 0, kAgent));
+            ls[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(all_parts, at + (uint32_t)(TILE * D + TILE + r) * 4u, 0, kAgent));
+            u[i] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(all_parts, at + (uint32_t)(r * D + 8 * ch) * 4u, 0, kAgent));
+            v[i] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(all_parts, at + (uint32_t)(r * D + 8 * ch + 4) * 4u, 0, kAgent));
           }
-        if (gp == 1) {
-          if (mine) write_row(r, ch, y0, y1, ref, l);
-          continue;
+          const float old = ref;
+#pragma unroll
+          for (int i = 0; i < MP; ++i)
+            if (p + i * gp < parts) ref = fmaxf(ref, ms[i]);
+          const float fin = ref == ninf ? 0.f : ref;
+          const float alpha = __builtin_amdgcn_exp2f(old - fin);
+          l *= alpha;
+          y0 *= alpha;
+          y1 *= alpha;
+#pragma unroll
+          for (int i = 0; i < MP; ++i) {
+            if (p + i * gp >= parts) continue;
+            const float w = __builtin_amdgcn_exp2f(ms[i] - fin);
+            l = fmaf(ls[i], w, l);
+            y0 += u[i] * w;
+            y1 += v[i] * w;
+          }
         }
-        if (base) __syncthreads();
+      if (gp == 1) {
+        if (mine) write_row(r, ch, y0, y1, ref, l);
+      } else {
         *reinterpret_cast<f32x4_t *>(&g_o[grp][8 * ch]) = y0;
         *reinterpret_cast<f32x4_t *>(&g_o[grp][8 * ch + 4]) = y1;
         if (ch == 0) {
@@ -682,7 +666,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   }
   if constexpr (kSplit) __syncthreads();  // (the LDS is free for the next tile)
   }
-  if (!kSplit || sh.most) return;
+  if (!kSplit || sh.part_log) return;
   tile0 += 2 * len + 512 / ROWB;
   if (tile0 >= cut1) return;
   if (++number >= n_seq) {
@@ -701,20 +685,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   }
 }
 
-// Rows a sequence and key head, on average, that this kernel is for.
-constexpr int kFewRowsMean = 64;
-bool cache_attn_few(int B, int H, int T, int Hq) { return (long long)T * (Hq / H) <= (long long)kFewRowsMean * B; }
-static int row_groups(int B, int H, int T, int Hq) { return (long long)T * (Hq / H) <= 16ll * B ? 1 : 2; }
-
+// Rows a sequence and key head, on average, that this kernel is for: those of one tile.  us of this kernel and of the one for
+// tiles of 128 rows (cache_attn.hip): 16 rows: one sequence of 2000 keys, two heads 12.6 / 16.1, of 30000, eight heads 44.6 / 47.7, 16 of
+// 4000 48.9 / 51.8, in e4m3 31.4 / 39.4, 64 of 1000 44.8 / 43.3, in e4m3 27.2 / 31.6; 24 rows (two tiles): 18 to 35 % slower
+// than that where one sequence is divided, 5 % faster to 9 % slower in batches.
+bool cache_attn_few(int B, int H, int T, int Hq) { return (long long)T * (Hq / H) <= (long long)kFewTile * B; }
 static bool few_divides(int B, long long items) { return B <= kSplitSeqs && items <= kFewItems; }
 
 size_t cache_attn_few_workspace_bytes(int B, int H, int D, int T, int Hq) {
-  const int nr = row_groups(B, H, T, Hq);
-  if (!few_divides(B, most_items(16 * nr, B, H, T, Hq))) return 0;
-  return 2 * (size_t)kFewPlaces * (sizeof(unsigned long long) + (size_t)(16 * nr * (D + 2)) * sizeof(float));
+  if (!few_divides(B, most_items(kFewTile, B, H, T, Hq))) return 0;
+  return 2 * (size_t)kFewPlaces * (sizeof(unsigned long long) + (size_t)(kFewTile * (D + 2)) * sizeof(float));
 }
 
-template <int D, bool kCodes, int NR>
+template <int D, bool kCodes>
 static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
@@ -727,14 +710,13 @@ static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, st, c);
     return check_launch("cache_attn_few_kernel");
   };
-  if (!split) return run(cache_attn_few_kernel<D, kCodes, NR, 0>);
-  return c.s.B <= 64 ? run(cache_attn_few_kernel<D, kCodes, NR, 1>) : run(cache_attn_few_kernel<D, kCodes, NR, kSplitSeqs / 64>);
+  if (!split) return run(cache_attn_few_kernel<D, kCodes, 0>);
+  return c.s.B <= 64 ? run(cache_attn_few_kernel<D, kCodes, 1>) : run(cache_attn_few_kernel<D, kCodes, kSplitSeqs / 64>);
 }
 
 int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, void *workspace, hipStream_t st) {
   const bool codes = hc.type == HEART_CACHE_E4M3;
-  const int nr = row_groups(hc.B, hc.H, T, Hq);
-  const long long items = most_items(16 * nr, hc.B, hc.H, T, Hq);
+  const long long items = most_items(kFewTile, hc.B, hc.H, T, Hq);
   if (items > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   const long long stages = ((long long)a.s.cap + kFewStage - 1) / kFewStage;
   const bool split = workspace && few_divides(hc.B, items) && stages <= (1ll << 27) / items;  // (sums of lengths fit 32 bits)
@@ -746,16 +728,8 @@ int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, voi
     a.part = (float *)(a.flags + 2 * kFewPlaces);
     a.mark = call_mark();
   }
-  auto go = [&](auto d, auto n) -> int {
-    constexpr int D = decltype(d)::value, NR = decltype(n)::value;
-    return codes ? launch_few_t<D, true, NR>(a, split, grid, st) : launch_few_t<D, false, NR>(a, split, grid, st);
-  };
-  const std::integral_constant<int, 128> d128;
-  const std::integral_constant<int, 64> d64;
-  const std::integral_constant<int, 1> one;
-  const std::integral_constant<int, 2> two;
-  if (hc.D == 128) return nr == 1 ? go(d128, one) : go(d128, two);
-  return nr == 1 ? go(d64, one) : go(d64, two);
+  if (hc.D == 128) return codes ? launch_few_t<128, true>(a, split, grid, st) : launch_few_t<128, false>(a, split, grid, st);
+  return codes ? launch_few_t<64, true>(a, split, grid, st) : launch_few_t<64, false>(a, split, grid, st);
 }
 
 }  // namespace heart
