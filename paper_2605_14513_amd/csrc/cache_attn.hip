@@ -42,10 +42,12 @@ constexpr int kPartFloats = 64 * (D / 2) + 128;
 // tiles, so that workgroups that read the same keys are neighbours.  Parts have at most L stages, the least L with which
 // there are no more parts than places, or than twice the places where that ends sooner (300 tiles of one length: two rounds
 // of thirds, not one round of wholes in 300 of 512 places): found from the lengths by every wavefront on its own.
+// (NB: sequences a lane.  One where that is enough: code that is jumped over has to be fetched all the same.)
+template <int NB>
 __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_slot, int lane, Work &k) {
-  constexpr int NB = kSplitSeqs / 64;
   int wgs[NB], st[NB];  // tiles of all heads, stages of a tile
-  int most = 1;
+  int most = 1, tiles = 0;
+  float all = 0.f;
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
     const int b = j * 64 + lane;
@@ -56,18 +58,30 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
       wgs[j] = tiles_of<kTile>(c, s) * c.H;
       st[j] = stages_of<kTile, kStage>(c, s);
       most = max(most, wgs[j] ? st[j] : 1);
+      tiles += wgs[j];
+      all += (float)wgs[j] * (float)st[j];
     }
   }
-  most = (int)wave_max_u32((uint32_t)most);
+  most = __builtin_amdgcn_readfirstlane((int)wave_max_u32((uint32_t)most));
+  tiles = __builtin_amdgcn_readfirstlane(wave_sum_i32(tiles));
+  all = wave_sum_f32(all);
+  // parts of a tile: st / L rounded up, or, by the rounding of the quotient, one more or less of many
+  auto parts_of = [&](int j, float inv) -> int { return (int)fmaf((float)(st[j] - 1), inv, 1.f); };
   auto count = [&](int L) -> int {
+    const float inv = __builtin_amdgcn_rcpf((float)L);
     int n = 0;
 #pragma unroll
     for (int j = 0; j < NB; ++j)
-      if (j * 64 < c.s.B) n += wgs[j] * (int)((unsigned)(st[j] + L - 1) / (unsigned)L);
+      if (j * 64 < c.s.B) n += wgs[j] * parts_of(j, inv);
     return __builtin_amdgcn_readfirstlane(wave_sum_i32(n));
   };
-  auto least = [&](int hi, int places) -> int {
-    int lo = min(kMinStages, hi);
+  // the least L with at most `places` parts, which are between all / L and all / L + tiles
+  auto least = [&](int places) -> int {
+    const int up = __builtin_amdgcn_readfirstlane((int)(all / (float)places));
+    const int room = places - tiles;
+    int lo = min(max(up, kMinStages), most);
+    int hi = room > 0 ? min(__builtin_amdgcn_readfirstlane((int)(all / (float)room)) + 2, most) : most;
+    hi = max(hi, lo);
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (count(mid) <= places) hi = mid;
@@ -75,30 +89,33 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
     }
     return lo;
   };
-  int lo = least(most, kPlaces);
-  if (c.rounds > 1 && lo > kPartCost) {
-    const int two = least(lo, 2 * kPlaces);
-    if (2 * two + kPartCost < lo) lo = two;
+  int L = least(kPlaces), total = count(L), room = kPlaces;
+  if (c.rounds > 1 && L > kPartCost) {
+    const int two = least(2 * kPlaces);
+    if (2 * two + kPartCost < L) L = two, total = count(L), room = 2 * kPlaces;
   }
+  // (one part each: the quotients' rounding let a part too many through, or token ranges overlap)
+  if (total > room) L = 0x3fffffff, total = count(L);
   // XCD x has the x-th eighth of the parts
-  const int total = count(lo), w = w_xcd * total / kNumXcd + w_slot;
+  const int w = w_xcd * total / kNumXcd + w_slot;
   if (w >= (w_xcd + 1) * total / kNumXcd) return false;
+  const float inv = __builtin_amdgcn_rcpf((float)L);
   int at = 0;
 #pragma unroll
   for (int j = 0; j < NB; ++j)
     if (j * 64 < c.s.B) {
-      const int parts = (int)((unsigned)(st[j] + lo - 1) / (unsigned)lo), n = wgs[j] * parts;
+      const int parts = parts_of(j, inv), n = wgs[j] * parts;
       const int end = at + wave_scan_i32(n), start = end - n;
       const unsigned long long here = __ballot(start <= w && w < end);
       if (here) {
         const int l = __ffsll((long long)here) - 1;
         k.b = j * 64 + l;
         k.parts = __builtin_amdgcn_readlane(parts, l);
-        k.step = __builtin_amdgcn_readlane(wgs[j], l) / c.H;  // tiles
-        const int r = w - __builtin_amdgcn_readlane(start, l);
-        k.h = r / (k.parts * k.step);
-        k.part = r / k.step % k.parts;
-        k.m = r % k.step;
+        k.step = (int)((unsigned)__builtin_amdgcn_readlane(wgs[j], l) / (unsigned)c.H);  // tiles
+        const unsigned r = (unsigned)(w - __builtin_amdgcn_readlane(start, l)), q = k.step == 1 ? r : r / (unsigned)k.step;
+        k.m = (int)(r - q * (unsigned)k.step);
+        k.h = (int)(q / (unsigned)k.parts);
+        k.part = (int)q - k.h * k.parts;
       }
       at = __builtin_amdgcn_readlane(end, 63);
     }
@@ -108,7 +125,7 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
 
 // kWhole: a workgroup per tile.  kParts: find_part.  kTail: the tiles of a last round that would not fill the places are
 // divided, c.tail parts each.
-enum CacheMode { kWhole, kParts, kTail };
+enum CacheMode { kWhole, kParts, kPartsWide, kTail };  // (kPartsWide: of more than 64 sequences)
 // Tile and key head of item i, of n_items = tiles H.  Where there are eight heads or a multiple, an XCD (workgroups are dealt to
 // them in turn) has every eighth head, one after the other, so that its workgroups find each other's keys in its L2 (40 heads
 // of 32760 keys in e4m3: 3000 to 3090 us, 3100 to 3130 with all heads at once).
@@ -154,8 +171,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   Work wk{0, 0, 0, 0, 1, 1, 0};
   constexpr bool kSplit = kMode != kWhole;
   int rec = 0;  // (divided keys) where to note the tile's parts
-  if constexpr (kMode == kParts) {
-    if (!find_part(c, (int)(blockIdx.x % kNumXcd), (int)(blockIdx.x / kNumXcd), lane, wk)) return;
+  constexpr bool kInParts = kMode == kParts || kMode == kPartsWide;
+  if constexpr (kInParts) {
+    if (!find_part<kMode == kParts ? 1 : kSplitSeqs / 64>(c, (int)(blockIdx.x % kNumXcd), (int)(blockIdx.x / kNumXcd), lane, wk))
+      return;
   } else {
     int i = (int)blockIdx.x, tile;
     if constexpr (kMode == kTail) {
@@ -179,7 +198,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   const Seq s = seq_of(c, wk.b);
   const int tiles = tiles_of<kTile>(c, s);
   if (wk.m < 0 || wk.m >= tiles) return;
-  if constexpr (kMode == kParts) rec = (tile_start<kTile>(c, wk.b) + wk.m) * c.H + wk.h;
+  if constexpr (kInParts) rec = (tile_start<kTile>(c, wk.b) + wk.m) * c.H + wk.h;
   else wk.m = tiles - 1 - wk.m;  // (later tiles see more keys: first)
   const int rows = s.n * c.G, r0 = wk.m * kTile;
   int lo, hi, first_key, end_key, ignore;
@@ -191,7 +210,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   if constexpr (kSplit) {
     const int per = max((n_stage + wk.parts - 1) / wk.parts, kMode == kTail ? 2 * kPartCost : 1);
     parts = max((n_stage + per - 1) / per, 1);
-    if (wk.part == 0 && t == 0 && (kMode == kParts || wk.parts > 1)) c.items[rec] = int4{wk.slot, parts, wk.step, 0};
+    if (wk.part == 0 && t == 0 && (kInParts || wk.parts > 1)) c.items[rec] = int4{wk.slot, parts, wk.step, 0};
     if (wk.part >= parts) return;
     stage0 += wk.part * per;
     n_stage = min(per, n_stage - wk.part * per);
@@ -738,7 +757,9 @@ static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
   };
   if (d.mode == kWhole) return run(cache_attn_kernel<D, kCodes, kWhole>, c.n_items);
   if (d.mode == kParts) {
-    if (int rc = run(cache_attn_kernel<D, kCodes, kParts>, d.slots())) return rc;
+    const int rc = c.s.B <= 64 ? run(cache_attn_kernel<D, kCodes, kParts>, d.slots())
+                               : run(cache_attn_kernel<D, kCodes, kPartsWide>, d.slots());
+    if (rc) return rc;
     hipLaunchKernelGGL((cache_attn_merge_kernel<D, kParts>), dim3((unsigned)(c.n_items * 4)), dim3(D * 2), 0, st, c);
   } else {
     if (int rc = run(cache_attn_kernel<D, kCodes, kTail>, c.whole + d.slots())) return rc;
