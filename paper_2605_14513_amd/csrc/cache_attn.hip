@@ -788,9 +788,13 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   if (items > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   Division d = divide(c.B, items);
   // (sequences so short that a second round of parts, and the launch that adds them up, gain nothing: causal attention of 4680 tokens
-  // to themselves, 8 heads 87 us whole, 93 divided, 16 heads 124, 129)
-  const bool brief = a.s.cap <= kBrief && (d.mode == kTail || d.rounds > 1);
-  if (!workspace || brief) d = {kWhole, 1, 0, 1, 0};
+  // to themselves, 8 heads 87 us whole, 93 divided, 16 heads 124, 129.  16 sequences of 4000 tokens and 48 queries, eight heads in
+  // e4m3: 77 whole, 44 in one round of parts)
+  if (a.s.cap <= kBrief) {
+    if (d.mode == kTail || (c.B == 1 && 2 * items > kPlaces)) d = {kWhole, 1, 0, 1, 0};
+    d.rounds = 1;
+  }
+  if (!workspace) d = {kWhole, 1, 0, 1, 0};
   a.n_items = (int)items;
   a.rounds = d.rounds;
   a.whole = d.whole;
