@@ -17,7 +17,8 @@
 // Stages.  K stage i holds slices 2i, 2i + 1; V stage i slices 2i - 1, 2i, so that one barrier per 64 keys retires both. Each
 // of the four wavefronts brings 16 rows of a stage, and pages hold a multiple of 16 tokens, so a wavefront needs one
 // page for a stage: a buffer descriptor over the rows that are there (rows that no query of the tile sees, from kv_len on
-// in any case, and pages that the table does not name, are out of its range and arrive as zeros).  The page ids of 64 stages lie in one register, a lane each.
+// in any case, and pages that the table does not name, are out of its range and arrive as zeros).  The page ids of 64
+// stages lie in one register, a lane each.
 //   bf16: LDS-direct loads, double-buffered, two slices ahead.
 //   e4m3: the codes are loaded into registers a stage earlier still and written to LDS as the bf16 values that they
 //     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
@@ -31,7 +32,7 @@ namespace heart {
 constexpr int kTile = 128;      // rows of a workgroup
 constexpr int kStage = 64;      // keys of a stage
 constexpr int kPlaces = 512;    // places for workgroups: two a CU
-constexpr int kMinStages = 4;   // fewest stages of a part
+constexpr int kMinStages = 4;   // fewest stages of a part (8 queries of 32000 keys, 3 key heads: 28 us, 31 with 2 or 3)
 constexpr int kPartCost = 8;    // what a part costs beside its stages (launch, first loads, 64 KB written and read), in stages
 
 // floats of one wavefront's part: accumulators, reference exponent and row sum of every lane
@@ -635,12 +636,20 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   }
 }
 
-// Adds up the parts of the tiles whose keys were divided: a wavefront for 32 rows and 32 columns, lanes as above.
-// Bound by latency (the parts come from the L2s and the memory-side cache): four parts at a time.
+constexpr int kMergeGroups = 4, kMergeParts = 4;  // groups, parts of a group in flight
+
+// Adds up the parts of the tiles whose keys were divided: a workgroup has 32 rows, a wavefront 32 columns, lanes as above.
+// Bound by latency (the parts come from the L2s and the memory-side cache): the parts are dealt to four groups of
+// wavefronts, four parts at a time each, and the groups' sums meet in LDS (8 queries of 32000 keys, 3 key heads in 125
+// parts each, D = 64: the call takes 28 us, 53 with one group).
 template <int D, CacheMode kMode>
-__global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall c) {
+__global__ __launch_bounds__(D * 2 * kMergeGroups) void cache_attn_merge_kernel(const AttnCall c) {
   constexpr float ninf = -__builtin_inff();
-  const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
+  constexpr int DT = D / 32, NP = kMergeParts;
+  __shared__ float meet[kMergeGroups - 1][DT][18][64];
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+  const int dt = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) % DT);
+  const int group = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) / DT);
   const int wave = (int)(blockIdx.x % 4), item = (int)(blockIdx.x / 4);
   int tile, h;
   if constexpr (kMode == kTail) item_at(c, c.whole + item, c.n_items, tile, h);
@@ -659,12 +668,12 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
   f32x4_t o[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) o[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < it.y; s0 += 4) {
-    float ms[4], ls[4];
-    f32x4_t x[4][4];
+  for (int s0 = group; s0 < it.y; s0 += kMergeGroups * NP) {
+    float ms[NP], ls[NP];
+    f32x4_t x[NP][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float *src = c.part + ((size_t)(it.x + min(s0 + i, it.y - 1) * it.z) * 4 + wave) * kPartFloats<D>;
+    for (int i = 0; i < NP; ++i) {
+      const float *src = c.part + ((size_t)(it.x + min(s0 + kMergeGroups * i, it.y - 1) * it.z) * 4 + wave) * kPartFloats<D>;
       ms[i] = src[64 * (D / 2) + lane];
       ls[i] = src[64 * (D / 2) + 64 + lane];
       const f32x4_t *o4 = reinterpret_cast<const f32x4_t *>(src) + 4 * 64 * dt + lane;
@@ -673,8 +682,8 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
     }
     const float old = ref;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (s0 + i < it.y) ref = fmaxf(ref, ms[i]);
+    for (int i = 0; i < NP; ++i)
+      if (s0 + kMergeGroups * i < it.y) ref = fmaxf(ref, ms[i]);
     // (a part whose logits are all -inf keeps the reference -inf: its weight is 0)
     const float fin = ref == ninf ? 0.f : ref;
     const float alpha = __builtin_amdgcn_exp2f(old - fin);
@@ -682,8 +691,8 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
 #pragma unroll
     for (int g = 0; g < 4; ++g) o[g] *= alpha;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (s0 + i >= it.y) continue;
+    for (int i = 0; i < NP; ++i) {
+      if (s0 + kMergeGroups * i >= it.y) continue;
       const float w = __builtin_amdgcn_exp2f(ms[i] - fin);
       l = fmaf(ls[i], w, l);
 #pragma unroll
@@ -691,6 +700,29 @@ __global__ __launch_bounds__(D * 2) void cache_attn_merge_kernel(const AttnCall 
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[g][e] = fmaf(x[i][g][e], w, o[g][e]);
     }
+  }
+  if (group) {
+    float(*to)[64] = meet[group - 1][dt];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[4 * g + e][lane] = o[g][e];
+    to[16][lane] = ref;
+    to[17][lane] = l;
+  }
+  __syncthreads();
+  if (group) return;
+#pragma unroll
+  for (int j = 0; j < kMergeGroups - 1; ++j) {
+    const float(*from)[64] = meet[j][dt];
+    const float other = from[16][lane], top = fmaxf(ref, other), fin = top == ninf ? 0.f : top;
+    const float a = __builtin_amdgcn_exp2f(ref - fin), b2 = __builtin_amdgcn_exp2f(other - fin);
+    ref = top;
+    l = fmaf(from[17][lane], b2, l * a);
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[g][e] = fmaf(from[4 * g + e][lane], b2, o[g][e] * a);
   }
   const float l_tot = l + __shfl_xor(l, 32, 64);
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
@@ -760,10 +792,10 @@ static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
     const int rc = c.s.B <= 64 ? run(cache_attn_kernel<D, kCodes, kParts>, d.slots())
                                : run(cache_attn_kernel<D, kCodes, kPartsWide>, d.slots());
     if (rc) return rc;
-    hipLaunchKernelGGL((cache_attn_merge_kernel<D, kParts>), dim3((unsigned)(c.n_items * 4)), dim3(D * 2), 0, st, c);
+    hipLaunchKernelGGL((cache_attn_merge_kernel<D, kParts>), dim3((unsigned)(c.n_items * 4)), dim3(D * 2 * kMergeGroups), 0, st, c);
   } else {
     if (int rc = run(cache_attn_kernel<D, kCodes, kTail>, c.whole + d.slots())) return rc;
-    hipLaunchKernelGGL((cache_attn_merge_kernel<D, kTail>), dim3((unsigned)((c.n_items - c.whole) * 4)), dim3(D * 2), 0, st, c);
+    hipLaunchKernelGGL((cache_attn_merge_kernel<D, kTail>), dim3((unsigned)((c.n_items - c.whole) * 4)), dim3(D * 2 * kMergeGroups), 0, st, c);
   }
   return check_launch("cache_attn_merge_kernel");
 }
