@@ -366,7 +366,8 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * out = softmax(scale q.k) v over these; scale <= 0 means 1/sqrt(D); lse fp32 [Hq,T] contiguous or NULL: natural
  * log-sum-exp of the scaled logits.  A query without keys gives zeros (lse = -inf).
  * Precision as heart_block_sparse_attn: bf16 products, fp32 sums, logits scaled and exponentiated in fp32, weights rounded
- * to bf16 for the second contraction (the row sum adds them unrounded).  Cached rows of 8 bits enter as the bf16 values
+ * to bf16 for the second contraction (the row sum adds them unrounded), or, where a sequence has 16 rows (new tokens times G)
+ * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values
  * they stand for.  Rows from kv_len on may hold anything, pages of nobody too; a NaN or an infinity among the first kv_len
  * tokens may also reach queries that do not see it.  out must not overlap q.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at

@@ -197,7 +197,7 @@ int launch_cache_write(const heart_cache &c, int T, const void *k, const long lo
                        const long long vs[2], const int *cu_q, hipStream_t st) {
   const bool codes = c.type == HEART_CACHE_E4M3;
   const long long eb = codes ? 1 : 2, waves = ((long long)T + kRowsWave - 1) / kRowsWave * c.H;
-  if (waves > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_write: too many rows (T = %d, H = %d)", T, c.H);
+  if (waves > 4 * kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_write: too many rows (T = %d, H = %d)", T, c.H);
   const CacheSide sk{(const uint16_t *)k, ks[0], ks[1], (uint8_t *)c.k, c.k_exp, c.k_stride[0] * eb, c.k_stride[1] * eb,
                      c.k_stride[2] * eb};
   const CacheSide sv{(const uint16_t *)v, vs[0], vs[1], (uint8_t *)c.v, c.v_exp, c.v_stride[0] * eb, c.v_stride[1] * eb,
@@ -216,7 +216,7 @@ int launch_cache_read(const heart_cache &c, int N, void *k, const long long ks[3
   const bool codes = c.type == HEART_CACHE_E4M3;
   const long long eb = codes ? 1 : 2, cap = (long long)c.max_pages * c.page;
   const long long tiles = ((N < cap ? N : cap) + 4 * kRowsWave - 1) / (4 * kRowsWave);
-  if ((long long)c.B * c.H > 0x7fffffffLL / tiles)
+  if ((long long)c.B * c.H > kMostGroups / tiles)
     return fail(HEART_EUNSUPPORTED, "heart_cache_read: too many rows (B = %d, H = %d, N = %d)", c.B, c.H, N);
   const CacheOut ok{(const uint8_t *)c.k, c.k_exp, c.k_stride[0] * eb, c.k_stride[1] * eb, c.k_stride[2] * eb,
                     (uint16_t *)k, ks[0], ks[1], ks[2]};

@@ -23,8 +23,6 @@
 //   e4m3: the codes are loaded into registers a stage earlier still and written to LDS as the bf16 values that they
 //     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
 //     time than the products take.
-#include <type_traits>
-
 #include "cache_attn_device.h"
 
 namespace heart {
@@ -817,7 +815,7 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.D)) * 1.4426950408889634f;
   if (cache_attn_few(c.B, c.H, T, Hq)) return launch_cache_attn_few(c, T, Hq, a, workspace, st);
   const long long items = most_items(kTile, c.B, c.H, T, Hq);
-  if (items > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
+  if (items > kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   Division d = divide(c.B, items);
   // (sequences so short that a second round of parts, and the launch that adds them up, gain nothing: causal attention of 4680 tokens
   // to themselves, 8 heads 87 us whole, 93 divided, 16 heads 124, 129.  16 sequences of 4000 tokens and 48 queries, eight heads in

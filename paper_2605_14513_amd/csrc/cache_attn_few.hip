@@ -717,7 +717,7 @@ static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream
 int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, void *workspace, hipStream_t st) {
   const bool codes = hc.type == HEART_CACHE_E4M3;
   const long long items = most_items(kFewTile, hc.B, hc.H, T, Hq);
-  if (items > 0x7fffffffLL) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
+  if (items > kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   const long long stages = ((long long)a.s.cap + kFewStage - 1) / kFewStage;
   const bool split = workspace && few_divides(hc.B, items) && stages <= (1ll << 27) / items;  // (sums of lengths fit 32 bits)
   long long grid = items;

@@ -17,6 +17,8 @@ struct CacheSeqs {
   int page_shift, max_pages, n_pages;
 };
 
+constexpr long long kMostGroups = (1ll << 24) - 1;  // workgroups of 256 threads: a launch has less than 2^32 threads
+
 inline CacheSeqs cache_seqs(const heart_cache &c, int T, const int *cu_q) {
   return CacheSeqs{cu_q, c.kv_len, c.page_table, T, c.B, T / c.B, c.max_pages * c.page, __builtin_ctz((unsigned)c.page),
                    c.max_pages, c.n_pages};

@@ -131,3 +131,13 @@ def test_binding_refuses_cpu_tensors(lib):
         heart.heart_cache_attn(x, c, c, i[None], i, workspace="none")
     with pytest.raises(ValueError, match="n tokens"):
         heart.heart_cache_read(c, c, i[None], i, k=bf(1, 2, 5, 64), v=bf(1, 2, 5, 64), n=3)
+
+
+def test_a_launch_has_less_than_2_to_the_32_threads(lib):
+    # (a wavefront has 16 tokens of a head in writing; a workgroup 64 tokens in reading, 16 rows or more in attention)
+    c = cache(B=1, H=1, max_pages=1 << 26)
+    for name, call in calls(lib, c, T=1 << 30, Hq=1, N=1 << 30).items():
+        if name != "attn":  # (2^23 tiles of 128 rows)
+            assert call() == EUNSUPPORTED and b"too many rows" in lib.heart_last_error(), name
+    assert calls(lib, cache(B=1 << 24, H=1), T=1 << 24, Hq=1)["attn"]() == EUNSUPPORTED
+    assert b"grid too large" in lib.heart_last_error()
