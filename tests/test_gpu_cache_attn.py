@@ -176,3 +176,13 @@ def test_many_tiles_with_divided_keys(kind, D, H, n, kv, causal):
     b, lb = run(cache, H, [n], causal=causal, workspace=None, what="whole")
     c, lc = run(cache, H, [n], causal=causal, workspace="garbage", what="again")
     assert torch.equal(a, c) and torch.equal(la, lc)
+
+
+@pytest.mark.parametrize("kind,D", [("bf16", 64), ("bf16", 128), ("e4m3", 128)])
+@pytest.mark.parametrize("n,Hq", [(1, 1), (1, 6), (8, 8), (5, 40)])
+def test_many_parts(kind, D, n, Hq):
+    """One long sequence of one key head: more than 64 parts a tile, of tiles of 16 rows and of 128."""
+    cache = Cache([30011], 1, D, 256, kind, seed=Hq)
+    a, la = run(cache, Hq, [n], workspace="garbage", what="divided")
+    b, lb = run(cache, Hq, [n], workspace="garbage", what="again")
+    assert torch.equal(a, b) and torch.equal(la, lb)

@@ -111,6 +111,25 @@ def test_captured_steps_follow_their_lengths(kind, n, H, Hq):
         assert (alone.float() - got.float()).abs().max() <= 2.0**-6 * max(1.0, got.float().abs().max().item())
 
 
+def test_captured_calls_share_a_workspace():
+    """Two captured calls of different shapes on one workspace, replayed in turn: each gives what it gives alone."""
+    caches = [Cache([4000, 300], 2, 128, 32, "bf16", seed=1), Cache([2500, 2600], 2, 128, 16, "e4m3", seed=2)]
+    qs = [torch.randn((2 * n, 8, 128), generator=torch.Generator().manual_seed(n)).bfloat16().cuda() for n in (1, 30)]
+    want = [heart.heart_cache_attn(q, *c.args(), **c.exps()) for q, c in zip(qs, caches)]
+    need = max(heart.heart_cache_attn_workspace_bytes(q, c.stored["k"], c.page_table) for q, c in zip(qs, caches))
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    out = [torch.zeros_like(q) for q in qs]
+    graphs = [torch.cuda.CUDAGraph() for _ in qs]
+    for i, c in enumerate(caches):
+        with torch.cuda.graph(graphs[i]):
+            heart.heart_cache_attn(qs[i], *c.args(), out=out[i], workspace=ws, **c.exps())
+    for turn in (0, 1, 0, 0, 1, 1, 0):
+        out[turn].zero_()
+        graphs[turn].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[turn], want[turn]), turn
+
+
 def test_two_streams_at_once():
     """Calls that overlap, each with a workspace of its own, give what they give alone."""
     caches = [Cache([4000, 300], 2, 128, 32, "bf16", seed=1), Cache([2500, 2600], 2, 64, 16, "e4m3", seed=2)]
