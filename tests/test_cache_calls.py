@@ -4,6 +4,8 @@ import ctypes
 import pytest
 import torch
 
+from test_kernel_resources import scratch_of
+
 
 @pytest.fixture(scope="module")
 def lib():
@@ -141,3 +143,9 @@ def test_a_launch_has_less_than_2_to_the_32_threads(lib):
             assert call() == EUNSUPPORTED and b"too many rows" in lib.heart_last_error(), name
     assert calls(lib, cache(B=1 << 24, H=1), T=1 << 24, Hq=1)["attn"]() == EUNSUPPORTED
     assert b"grid too large" in lib.heart_last_error()
+
+
+@pytest.mark.parametrize("source", ["cache.hip", "cache_attn.hip", "cache_attn_few.hip"])
+def test_cache_kernels_use_no_scratch_memory(source):
+    sizes = scratch_of(source)
+    assert not any(sizes.values()), sizes
