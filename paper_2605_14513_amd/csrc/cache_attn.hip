@@ -23,6 +23,10 @@
 //   e4m3: the codes are loaded into registers a stage earlier still and written to LDS as the bf16 values that they
 //     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
 //     time than the products take.
+//
+// Bound by the matrix instructions and the power that they draw.  PFLOP/s: 4680 queries of 12 heads over 32760 keys in bf16
+// 1.03 to 1.07 (matrix pipes busy 59 % of the cycles), of 40 heads in e4m3 0.99 to 1.02 (53 %: the conversions); a bf16 matrix
+// product of 8192^3 1.20.  Calls of few tiles are bound by latency: 16 sequences with 8 drafts of 24 heads, window 4096, 20 us.
 #include "cache_attn_device.h"
 
 namespace heart {
