@@ -369,7 +369,8 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * to bf16 for the second contraction (the row sum adds them unrounded), or, where a sequence has 16 rows (new tokens times G)
  * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values
  * they stand for.  Rows from kv_len on may hold anything, pages of nobody too; a NaN or an infinity among the first kv_len
- * tokens may also reach queries that do not see it.  out must not overlap q.
+ * tokens may also reach queries that do not see it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v|
+ * over a query's keys has to stay below 2^128.)  out must not overlap q.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
  * B, H, D alone), or NULL.  With it the keys of few queries are divided over the chip, into parts that depend on all
  * lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on

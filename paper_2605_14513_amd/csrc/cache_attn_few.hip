@@ -16,7 +16,8 @@
 // Dividing the keys: struct Shares.  The workgroup that finds all parts of a tile there adds them up.
 //
 // 64 ragged sequences of up to 8192 tokens, 8 key heads of 128, e4m3 (385 MB) 74 us, 5.2 TB/s; one of 120001 tokens, bf16 (492 MB)
-// 84 us, 5.8 TB/s; 4.3 GB 6.9 TB/s (a plain read 7.1).  One of 1000 tokens, two heads: 9.9 us, bound by latency.
+// 84 us, 5.8 TB/s; 64 of 16384, bf16 (4.3 GB) 6.8 TB/s, of 32768 in e4m3 6.6 (a plain read 7.1).  One of
+// 1000 tokens, two heads: 9.9 us, bound by latency.
 #include "cache_attn_device.h"
 
 namespace heart {
