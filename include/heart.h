@@ -323,7 +323,8 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
  * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
  * call's tensors (NULL: each has T/B of them), and the last of them is at position kv_len[b]-1.  Tokens behind cu_q[B], and
- * output rows of them, are left alone.  cu_q must not fall and lie in [0, T]; else tokens may be left out.
+ * output rows of them, are left alone.  cu_q must not fall and lie in [0, T]; else tokens may be left out, or taken as those of
+ * another of the sequences whose ranges they are in.
  * Nothing that these arrays hold leaves the tensors: a position below 0 or from max_pages * page on is neither written nor
  * read nor seen, and a page outside [0, n_pages) is not written and reads as zeros.  Sequences may share pages that no call
  * writes; of two new tokens at one place of the cache, either or a mixture is kept.

@@ -51,6 +51,7 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
   int wgs[NB], st[NB];  // tiles of all heads, stages of a tile
   int most = 1, tiles = 0;
   float all = 0.f;
+  bool falls = false;
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
     const int b = j * 64 + lane;
@@ -58,12 +59,20 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
     st[j] = 1;
     if (j * 64 < c.s.B && b < c.s.B) {
       const Seq s = seq_of(c, b);
+      falls = falls || (c.s.cu && c.s.cu[b + 1] < c.s.cu[b]);
       wgs[j] = tiles_of<kTile>(c, s) * c.H;
       st[j] = stages_of<kTile, kStage>(c, s);
       most = max(most, wgs[j] ? st[j] : 1);
       tiles += wgs[j];
       all += (float)wgs[j] * (float)st[j];
     }
+  }
+  // Token ranges that fall somewhere overlap: there can be more tiles than places, and records that nobody writes, though the merge
+  // finds their tiles.  No work then, and records of no parts for all tiles that the merge can find (fewer than kPlaces).
+  if (__any(falls)) {
+    const int i = w_slot * kNumXcd + w_xcd;
+    if (i < kPlaces && threadIdx.x == 0) c.items[i] = int4{0, 0, 0, 0};
+    return false;
   }
   most = __builtin_amdgcn_readfirstlane((int)wave_max_u32((uint32_t)most));
   tiles = __builtin_amdgcn_readfirstlane(wave_sum_i32(tiles));
@@ -97,7 +106,7 @@ __device__ __forceinline__ bool find_part(const AttnCall &c, int w_xcd, int w_sl
     const int two = least(2 * kPlaces);
     if (2 * two + kPartCost < L) L = two, total = count(L), room = 2 * kPlaces;
   }
-  // (one part each: the quotients' rounding let a part too many through, or token ranges overlap)
+  // (one part each: the quotients' rounding let a part too many through)
   if (total > room) L = 0x3fffffff, total = count(L);
   // XCD x has the x-th eighth of the parts
   const int w = w_xcd * total / kNumXcd + w_slot;
