@@ -107,7 +107,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheSide k, CacheSide
     first = b * s.per;
   }
   int page = -1, off = 0;
-  if (lane < kRowsWave && t < s.T && b < s.B && t >= first) {
+  // (where ranges fall, the number of ends need not be that of a sequence that has the token)
+  if (lane < kRowsWave && t < s.T && b < s.B && t >= first && t - first < n) {
     const long long pos = (long long)s.kv_len[b] - n + (t - first);
     if (pos >= 0 && pos < s.cap) {
       page = cache_page(s, b, (int)pos);

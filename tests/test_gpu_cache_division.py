@@ -45,3 +45,27 @@ def test_ranges_that_fall_leave_tokens_out(cu, T, H, G, kind, D):
     heart.heart_cache_attn(q, *c.args(), cu_q=cu_of(cu), out=out, lse=lse, workspace=None, **c.exps())
     torch.cuda.synchronize()
     assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("cu", [[0, 9, 2, 3], [0, 40, 0, 40], [30, 10, 20, 5], [0, 7, -3, 12], [5, 2**31 - 1, 3, 4], [-(2**31), 20, 1, 40]])
+def test_writing_by_ranges_that_fall_stays_behind_the_last_token(cu, kind):
+    """A token goes to a place among its sequence's new ones, or nowhere."""
+    c = Pages([100, 130, 90], 2, 64, 16, kind, room=300)
+    # (every position of the table has a page, so that one behind the last token could be written)
+    c.page_table = torch.arange(3 * 19, dtype=torch.int32, device="cuda").reshape(3, 19)
+    store = torch.zeros((57, 2, 16, 64), dtype=torch.uint8 if kind == "e4m3" else torch.bfloat16, device="cuda")
+    k, v = store.clone(), store.clone()
+    e = dict.fromkeys(("k_exp", "v_exp"))
+    if kind == "e4m3":
+        e = {n: torch.zeros((57, 2, 16), dtype=torch.uint8, device="cuda") for n in e}
+    x = torch.ones((40, 2, 64), dtype=torch.bfloat16, device="cuda")
+    print(f"cache_write ranges {cu} {kind}", flush=True)
+    heart.heart_cache_write(x, x, *((t.view(torch.float8_e4m3fn) if kind == "e4m3" else t) for t in (k, v)), c.page_table, c.kv_len,
+                            cu_q=cu_of(cu), **e)
+    torch.cuda.synchronize()
+    for t in (k, v):
+        there = (t != 0).any(-1).any(1).reshape(3, 19 * 16)
+        for b, kv in enumerate(c.kvs):
+            n = cu[b + 1] - cu[b]
+            assert not there[b, kv:].any() and not there[b, :max(kv - max(n, 0), 0)].any(), (b, there[b].nonzero().flatten().tolist())
