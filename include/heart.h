@@ -365,7 +365,7 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  *     ordinary causal attention; the tokens of a latent frame: frame after frame), and no keys for p < 0;
  *   window = 0: lo = 0;  window = w > 0: lo = max(0, hi - w).
  * out = softmax(scale q.k) v over these; scale <= 0 means 1/sqrt(D); lse fp32 [Hq,T] contiguous or NULL: natural
- * log-sum-exp of the scaled logits.  A query without keys gives zeros (lse = -inf).
+ * log-sum-exp of the scaled logits.  A query without keys gives zeros (lse = -inf), one with a logit of NaN or +inf NaN in both.
  * Precision as heart_block_sparse_attn: bf16 products, fp32 sums, logits scaled and exponentiated in fp32, weights rounded
  * to bf16 for the second contraction (the row sum adds them unrounded), or, where a sequence has 16 rows (new tokens times G)
  * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values

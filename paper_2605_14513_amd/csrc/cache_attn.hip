@@ -619,10 +619,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 
   // ---- epilogue: normalise, stage through LDS, coalesced bf16 store -----------------------
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // (a NaN stays one, in the log-sum-exp too)
   if (c.lse && hf == 0 && row < rows) {
     const Row at = row_of(c, s, wk.h, row);
-    c.lse[(long long)at.head * c.s.T + at.token] = l_tot > 0.f ? (m_ref + log2f(l_tot)) * 0.6931471805599453f : ninf;
+    c.lse[(long long)at.head * c.s.T + at.token] = l_tot == 0.f ? ninf : (m_ref + log2f(l_tot)) * 0.6931471805599453f;
   }
   uint16_t *sO = reinterpret_cast<uint16_t *>(smem);  // [kTile][SO]
 #pragma unroll
@@ -736,11 +736,11 @@ __global__ __launch_bounds__(D * 2 * kMergeGroups) void cache_attn_merge_kernel(
       for (int e = 0; e < 4; ++e) o[g][e] = fmaf(from[4 * g + e][lane], b2, o[g][e] * a);
   }
   const float l_tot = l + __shfl_xor(l, 32, 64);
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
   if (row >= rows) return;
   const Row at = row_of(c, s, h, row);
   if (c.lse && dt == 0 && hf == 0)
-    c.lse[(long long)at.head * c.s.T + at.token] = l_tot > 0.f ? (ref + log2f(l_tot)) * 0.6931471805599453f : ninf;
+    c.lse[(long long)at.head * c.s.T + at.token] = l_tot == 0.f ? ninf : (ref + log2f(l_tot)) * 0.6931471805599453f;
   uint16_t *dst = c.out + at.token * c.ot + at.head * c.oh + 32 * dt + 4 * hf;
 #pragma unroll
   for (int g = 0; g < 4; ++g) {

@@ -531,13 +531,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   __syncthreads();
   constexpr int CH = D / 8;  // threads of a row, 8 elements each
   auto write_row = [&](int r, int ch, f32x4_t y0, f32x4_t y1, float ref, float l) __attribute__((always_inline)) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one, in the log-sum-exp too)
     const Row at = at0.row(head, r);
     *reinterpret_cast<u32x4_t *>(c.out + at.token * c.ot + at.head * c.oh + 8 * ch) =
         u32x4_t{cvt_pk_bf16(y0[0] * inv, y0[1] * inv), cvt_pk_bf16(y0[2] * inv, y0[3] * inv),
                 cvt_pk_bf16(y1[0] * inv, y1[1] * inv), cvt_pk_bf16(y1[2] * inv, y1[3] * inv)};
     if (c.lse && ch == 0)
-      c.lse[(long long)at.head * c.s.T + at.token] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : ninf;
+      c.lse[(long long)at.head * c.s.T + at.token] = l == 0.f ? ninf : (ref + log2f(l)) * 0.6931471805599453f;
   };
   constexpr int kAgent = 16;  // (sc1: past the L2 of this XCD, where the workgroups of all XCDs meet)
   auto part_rsrc = [&](int slot) __attribute__((always_inline)) -> __amdgpu_buffer_rsrc_t {

@@ -1,0 +1,61 @@
+"""heart_cache_attn on values at the ends of the formats: NaN and infinities among what is seen, exponents of rows, weights that
+cancel."""
+import math
+
+import pytest
+import torch
+
+import paper_2605_14513_amd as heart
+from cache_reference import E4M3, Pages, near, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def new_q(T, Hq, D, seed=1):
+    return torch.randn((T, Hq, D), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").bfloat16()
+
+
+def place(c, b, j):
+    """Page and row of token j of sequence b."""
+    return c.page_table[b, j // c.page].item(), j % c.page
+
+
+# (few rows in parts, 128-row tiles in parts; with and without a workspace)
+@pytest.mark.parametrize("workspace", ["auto", None])
+@pytest.mark.parametrize("n", [2, 150])
+@pytest.mark.parametrize("kind,D", [("bf16", 128), ("bf16", 64), ("e4m3", 128)])
+def test_logits_that_are_not_finite(kind, D, n, workspace):
+    """A query with NaN among its logits gives NaN in out and in the log-sum-exp, not what one without keys gives; so does +inf; a
+    key whose logit is -inf has weight 0.  Other queries, and heads, get what they get without."""
+    H, G, kvs = 2, 2, [3000, 700]
+    c = Pages(kvs, H, D, 32, kind)
+    q = new_q(2 * n, H * G, D).abs()  # (signs: an infinite k gives an infinite logit)
+    q[n + 1, 3, D // 2] = math.nan
+    want, want_lse, tol, ltol = reference(c, q.nan_to_num(0.0), [n, n])
+    bad = torch.zeros((2 * n, H * G), dtype=torch.bool, device="cuda")
+    bad[n + 1, 3] = True
+    sees = torch.arange(n, device="cuda")
+    for b, h, j, x in ((0, 0, kvs[0] - 1, math.nan), (0, 1, kvs[0] - n, math.inf), (1, 0, 5, -math.inf)):
+        page, row = place(c, b, j)
+        if kind == "e4m3":  # (no infinities in the format)
+            if x == -math.inf:
+                continue
+            c.stored["k"][page, h, row] = math.nan
+        else:
+            c.stored["k"][page, h, row] = x
+        if x == -math.inf:  # the definition without that key
+            k, v = (c.sequence(m, 1)[h][torch.arange(kvs[1]) != j] for m in "kv")
+            for i in range(n):
+                for g in range(G):
+                    s = k[:kvs[1] - n + i] @ q[n + i, h * G + g].double() / math.sqrt(D)
+                    want[n + i, h * G + g] = torch.softmax(s, 0) @ v[:kvs[1] - n + i]
+                    want_lse[h * G + g, n + i] = torch.logsumexp(s, 0)
+        else:
+            bad[b * n:(b + 1) * n, h * G:(h + 1) * G] |= (kvs[b] - n + sees >= j)[:, None]
+    print(f"cache_attn not finite {kind} D={D} n={n} workspace={workspace}", flush=True)
+    out, lse = torch.zeros_like(q), torch.zeros((H * G, 2 * n), device="cuda")
+    heart.heart_cache_attn(q, *c.args(), out=out, lse=lse, workspace=workspace, **c.exps())
+    torch.cuda.synchronize()
+    assert out[bad].isnan().all() and lse.t()[bad].isnan().all()
+    near(out[~bad], want[~bad], tol[~bad], "out")
+    near(lse.t()[~bad], want_lse.t()[~bad], ltol.t()[~bad], "lse")
