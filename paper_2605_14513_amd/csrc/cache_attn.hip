@@ -27,6 +27,8 @@
 // Bound by the matrix instructions and the power that they draw.  PFLOP/s: 4680 queries of 12 heads over 32760 keys in bf16
 // 1.03 to 1.07 (matrix pipes busy 59 % of the cycles), of 40 heads in e4m3 0.99 to 1.02 (53 %: the conversions); a bf16 matrix
 // product of 8192^3 1.20.  Calls of few tiles are bound by latency: 16 sequences with 8 drafts of 24 heads, window 4096, 20 us.
+#include <type_traits>
+
 #include "cache_attn_device.h"
 
 namespace heart {
@@ -791,21 +793,22 @@ static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
   constexpr int lds = 4 * kStage * D * 2, staging = kTile * (D + 8) * 2, bytes = lds > staging ? lds : staging;
-  auto run = [&](auto kern, long long grid) -> int {
-    static DeviceFlags attr_set;
+  auto run = [&](auto mode, long long grid) -> int {
+    auto kern = cache_attn_kernel<D, kCodes, decltype(mode)::value>;
+    static DeviceFlags attr_set;  // per instantiation: the attribute is per function and device
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
       return fail(HEART_EHIP, "hipFuncSetAttribute(max dynamic LDS %d): %s", bytes, hipGetErrorString(e));
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, st, c);
     return check_launch("cache_attn_kernel");
   };
-  if (d.mode == kWhole) return run(cache_attn_kernel<D, kCodes, kWhole>, c.n_items);
+  if (d.mode == kWhole) return run(std::integral_constant<CacheMode, kWhole>{}, c.n_items);
   if (d.mode == kParts) {
-    const int rc = c.s.B <= 64 ? run(cache_attn_kernel<D, kCodes, kParts>, d.slots())
-                               : run(cache_attn_kernel<D, kCodes, kPartsWide>, d.slots());
+    const int rc = c.s.B <= 64 ? run(std::integral_constant<CacheMode, kParts>{}, d.slots())
+                               : run(std::integral_constant<CacheMode, kPartsWide>{}, d.slots());
     if (rc) return rc;
     hipLaunchKernelGGL((cache_attn_merge_kernel<D, kParts>), dim3((unsigned)(c.n_items * 4)), dim3(D * 2 * kMergeGroups), 0, st, c);
   } else {
-    if (int rc = run(cache_attn_kernel<D, kCodes, kTail>, c.whole + d.slots())) return rc;
+    if (int rc = run(std::integral_constant<CacheMode, kTail>{}, c.whole + d.slots())) return rc;
     hipLaunchKernelGGL((cache_attn_merge_kernel<D, kTail>), dim3((unsigned)((c.n_items - c.whole) * 4)), dim3(D * 2 * kMergeGroups), 0, st, c);
   }
   return check_launch("cache_attn_merge_kernel");

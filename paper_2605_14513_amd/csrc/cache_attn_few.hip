@@ -18,6 +18,8 @@
 // 64 ragged sequences of up to 8192 tokens, 8 key heads of 128, e4m3 (385 MB) 74 us, 5.2 TB/s; one of 120001 tokens, bf16 (492 MB)
 // 84 us, 5.8 TB/s; 64 of 16384, bf16 (4.3 GB) 6.8 TB/s, of 32768 in e4m3 6.6 (a plain read 7.1).  One of
 // 1000 tokens, two heads: 9.9 us, bound by latency.
+#include <type_traits>
+
 #include "cache_attn_device.h"
 
 namespace heart {
@@ -707,15 +709,16 @@ static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
   constexpr int bytes = 4 * FewShape<D, kCodes>::WAVE_B;
   static_assert(bytes >= (256 / (D / 8)) * (D + 2) * 4, "sums of the parts fit the LDS");
-  auto run = [&](auto kern) -> int {
-    static DeviceFlags attr_set;
+  auto run = [&](auto seqs) -> int {
+    auto kern = cache_attn_few_kernel<D, kCodes, decltype(seqs)::value>;
+    static DeviceFlags attr_set;  // per instantiation: the attribute is per function and device
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
       return fail(HEART_EHIP, "hipFuncSetAttribute(max dynamic LDS %d): %s", bytes, hipGetErrorString(e));
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, st, c);
     return check_launch("cache_attn_few_kernel");
   };
-  if (!split) return run(cache_attn_few_kernel<D, kCodes, 0>);
-  return c.s.B <= 64 ? run(cache_attn_few_kernel<D, kCodes, 1>) : run(cache_attn_few_kernel<D, kCodes, kSplitSeqs / 64>);
+  if (!split) return run(std::integral_constant<int, 0>{});
+  return c.s.B <= 64 ? run(std::integral_constant<int, 1>{}) : run(std::integral_constant<int, kSplitSeqs / 64>{});
 }
 
 int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, void *workspace, hipStream_t st) {
