@@ -317,8 +317,9 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  *   HEART_CACHE_BF16: elements are bf16; k_exp and v_exp are NULL.
  *   HEART_CACHE_E4M3: elements are 8 bits (e4m3 as in the OCP 8-bit floating point specification: finite up to 448, no
  *     infinities), and k_exp, v_exp uint8 [n_pages,H,page] (contiguous, 16-byte aligned) hold an exponent for each row of
- *     D: an element stands for code * 2^(exp - 127).  A power of two makes reading exact (codes have 4 significant bits) and
- *     leaves one rounding, to the nearest code, in writing.
+ *     D: an element stands for code * 2^(exp - 127), exp 0 .. 254 (rows under 255, which are never written, may give
+ *     anything).  A power of two makes reading exact (codes have 4 significant bits) and leaves one rounding, to the nearest
+ *     code, in writing.
  * B sequences: page_table int32 [B,max_pages] names the pages of each in order, kv_len int32 [B] says how many tokens it
  * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
  * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
@@ -368,10 +369,11 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * log-sum-exp of the scaled logits.  A query without keys gives zeros (lse = -inf), one with a logit of NaN or +inf NaN in both.
  * Precision as heart_block_sparse_attn: bf16 products, fp32 sums, logits scaled and exponentiated in fp32, weights rounded
  * to bf16 for the second contraction (the row sum adds them unrounded), or, where a sequence has 16 rows (new tokens times G)
- * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values
- * they stand for.  Rows from kv_len on may hold anything, pages of nobody too; a NaN or an infinity among the first kv_len
- * tokens may also reach queries that do not see it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v|
- * over a query's keys has to stay below 2^128.)  out must not overlap q.
+ * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values they stand for (as part
+ * of the weights, v's exponents, where these are two bf16: below an exponent of 32 they lose bits).  Rows from kv_len on may
+ * hold anything, pages of nobody too; a NaN or an infinity among the first kv_len tokens may also reach queries that do not see
+ * it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v| over a query's keys has to stay below 2^128.)  out
+ * must not overlap q.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
  * B, H, D alone), or NULL.  With it the keys of few queries are divided over the chip, into parts that depend on all
  * lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on

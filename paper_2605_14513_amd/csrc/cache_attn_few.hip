@@ -398,7 +398,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
           const float ku = unit_of(min((uint32_t)se[16 * n + l16] & named[0][n], 254u));
           const uint32_t ve = *reinterpret_cast<const uint32_t *>(se + 16 * NT + 16 * n + 4 * g) & named[0][n];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vu[n][e] = unit_of(min((ve >> (8 * e)) & 0xffu, 254u));
+          for (int e = 0; e < 4; ++e)  // (2^-127 is a subnormal number)
+            vu[n][e] = __uint_as_float(min(max(((ve >> (8 * e)) & 0xffu) << 23, 0x00400000u), 254u << 23));
 #pragma unroll
           for (int j = 0; j < KR; ++j) {
             const u32x4_t x = *reinterpret_cast<const u32x4_t *>(sk + 16 * n * ROWB + koff[j]);

@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t codes_to_bf16(uint32_t w, float unit) {
   const bf16x2_c r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, unit, kUpper);
   return __builtin_bit_cast(uint32_t, r);
 }
-// 2^(exp - 127); an exponent byte of 0 (rows that are not there) gives 0
+// 2^(exp - 127) as the conversions take it: by the exponent bits alone (0: 2^-127, though as a float it is 0; 255: NaN)
 __device__ __forceinline__ float unit_of(uint32_t exp) { return __uint_as_float(exp << 23); }
 
 }  // namespace heart

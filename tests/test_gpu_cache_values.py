@@ -59,3 +59,37 @@ def test_logits_that_are_not_finite(kind, D, n, workspace):
     assert out[bad].isnan().all() and lse.t()[bad].isnan().all()
     near(out[~bad], want[~bad], tol[~bad], "out")
     near(lse.t()[~bad], want_lse.t()[~bad], ltol.t()[~bad], "lse")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_under_every_exponent(D):
+    """Exponent bytes 0 to 254 are powers of two from 2^-127 on: read back, and attended by few rows and by many.  Every sequence
+    is one token whose v is a row under one exponent, so that out is that row; k is such a row too and q is zero."""
+    B, page = 255, 16
+    codes = (torch.arange(B * D, device="cuda") * 7 % 127).to(torch.uint8).reshape(B, D) | (torch.arange(D, device="cuda") % 2 * 128).to(torch.uint8)
+    exp = torch.arange(B, device="cuda", dtype=torch.uint8)
+    value = codes.view(E4M3).double() * torch.exp2(exp.double() - 127)[:, None]
+    want = value.bfloat16()  # (beyond the largest bf16: infinities)
+    store = torch.zeros((B, 1, page, D), dtype=torch.uint8, device="cuda")
+    e = torch.full((B, 1, page), 255, dtype=torch.uint8, device="cuda")
+    store[:, 0, 0], e[:, 0, 0] = codes, exp
+    plain = torch.full_like(e, 127)
+    table = torch.arange(B, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    one = torch.ones(B, dtype=torch.int32, device="cuda")
+    print(f"cache_read, cache_attn exponents D={D}", flush=True)
+    k, v = heart.heart_cache_read(store.view(E4M3), store.view(E4M3), table, one, n=1, k_exp=e, v_exp=e)
+    normal = (value.abs() >= 2.0**-126) | (value == 0)  # (those below may be read as zero)
+    for x in (k, v):
+        assert ((x[:, 0, 0] == want) | (~normal & (x[:, 0, 0] == 0))).all()
+    here = slice(0, 240)  # (2^8 sum |v| has to stay below 2^128)
+    for G in (1, 40):  # few rows, and tiles of 128
+        q = torch.zeros((B, G, D), dtype=torch.bfloat16, device="cuda")
+        out = heart.heart_cache_attn(q, store.view(E4M3), store.view(E4M3), table, one, k_exp=plain, v_exp=e)
+        for g in range(G):
+            assert ((out[here, g] == want[here]) | (~normal[here] & (out[here, g] == 0))).all(), g
+        # (as k: a query along one element has that logit)
+        q[:, :, 0] = 1.0
+        lse = torch.zeros((G, B), device="cuda")
+        heart.heart_cache_attn(q, store.view(E4M3), store.view(E4M3), table, one, k_exp=e, v_exp=plain, lse=lse, scale=1.0)
+        s = value[here, 0]
+        assert ((lse[:, here] - s).abs() <= 2.0**-20 * s.abs() + 2.0**-100).all()
