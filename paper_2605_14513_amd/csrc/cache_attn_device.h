@@ -65,15 +65,17 @@ __device__ __forceinline__ Seq seq_of(const AttnCall &c, int b) {
   s.len = min(kv, c.s.cap);
   return s;
 }
-// Keys lo .. hi - 1 that the query at position p sees.
+// Keys lo .. hi - 1 that the query at position p sees: of those by the length, the ones that there is room for.
 __device__ __forceinline__ void seen_by(const AttnCall &c, const Seq &s, int p, int &lo, int &hi) {
-  hi = s.len;
+  hi = s.pos0 + s.n;
   if (c.causal) {
     uint32_t end = (uint32_t)max(p, 0) + 1u;
     if (c.causal > 1) end = (end - 1u) / (uint32_t)c.causal * (uint32_t)c.causal + (uint32_t)c.causal;  // < 2^32
-    hi = p < 0 ? 0 : (int)min(end, (uint32_t)s.len);
+    hi = p < 0 ? 0 : (int)min(end, (uint32_t)hi);
   }
   lo = c.window ? max(0, hi - c.window) : 0;
+  hi = min(hi, s.len);
+  lo = min(lo, hi);
 }
 // Tiles of TILE rows.
 template <int TILE>

@@ -16,6 +16,7 @@ class Pages:
         g = torch.Generator(device="cuda").manual_seed(seed)
         r = random.Random(seed)
         self.kvs, self.H, self.D, self.page, self.kind = list(kvs), H, D, page, kind
+        self.lens = self.kvs  # (kv_len, which may be more than there is room for)
         need = [-(-n // page) for n in kvs]
         n_pages, M = sum(need) + 2, max(max(need), -(-room // page), 1)
         ids = list(range(n_pages))
@@ -77,16 +78,16 @@ def reference(pages, q, qs, causal=1, window=0, scale=0.0, chain=None, weight=2.
     lse, ltol = torch.full((Hq, T), -math.inf, **z), torch.zeros((Hq, T), **z)
     at = 0
     for b, n in enumerate(qs):
-        kv = pages.kvs[b]
+        kv, there = pages.lens[b], pages.kvs[b]
         if n and kv:
             k, v = pages.sequence("k", b), pages.sequence("v", b)
             p = torch.arange(kv - n, kv, device="cuda")
             hi = ((p // causal + 1) * causal).clamp_max(kv).masked_fill(p < 0, 0) if causal else torch.full_like(p, kv)
             lo = (hi - window).clamp_min(0) if window else torch.zeros_like(hi)
-            j = torch.arange(kv, device="cuda")
+            j = torch.arange(there, device="cuda")
             hidden = (j < lo[:, None]) | (j >= hi[:, None])
-            some = (hi > lo)[:, None]
-            c = kv if chain is None else chain
+            some = (hi.clamp_max(there) > lo)[:, None]
+            c = there if chain is None else chain
             for h in range(Hq):
                 x, kh, vh = q[at:at + n, h].double(), k[h // G], v[h // G]
                 s = (x @ kh.t() * scale).masked_fill(hidden, -math.inf)

@@ -93,3 +93,22 @@ def test_rows_under_every_exponent(D):
         heart.heart_cache_attn(q, store.view(E4M3), store.view(E4M3), table, one, k_exp=e, v_exp=plain, lse=lse, scale=1.0)
         s = value[here, 0]
         assert ((lse[:, here] - s).abs() <= 2.0**-20 * s.abs() + 2.0**-100).all()
+
+
+@pytest.mark.parametrize("kind,D", [("bf16", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("n", [3, 70])
+def test_windows_of_lengths_beyond_the_page_table(kind, D, n):
+    """kv_len past the room of the table: a window reaches back from the position, not from the last key that there is room for."""
+    c = Pages([256, 256, 256], 2, D, 16, kind)
+    c.lens = [256 + n // 2, 300, 1000]
+    c.kv_len = torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+    q = new_q(3 * n, 4, D)
+    for causal, window in ((1, 60), (0, 60), (0, 0), (64, 100), (1, 30), (1, 0), (1, 2000)):
+        want, want_lse, tol, ltol = reference(c, q, [n] * 3, causal, window)
+        assert causal == 0 or window != 60 or n != 70 or (want_lse == -math.inf).any()
+        for workspace in ("auto", None):
+            print(f"cache_attn beyond the table {kind} D={D} n={n} causal={causal} window={window} workspace={workspace}", flush=True)
+            lse = torch.zeros((4, 3 * n), device="cuda")
+            out = heart.heart_cache_attn(q, *c.args(), causal=causal, window=window, lse=lse, workspace=workspace, **c.exps())
+            near(out, want, tol, "out")
+            near(lse, want_lse, ltol, "lse")
