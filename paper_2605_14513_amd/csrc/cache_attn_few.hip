@@ -28,10 +28,11 @@ constexpr int kFewTile = 16;     // rows of a workgroup
 constexpr int kFewStage = 128;   // keys that shares are measured in
 constexpr int kFewMin = 2;       // shortest share, in stages
 constexpr int kFewCut = 1;       // fewest stages of a part: a cut closer to an end of its tile goes there
-// A call that reads more than this loads past the caches (nt): as nothing of it is read twice, and what the memory-side cache (256
-// MB) could keep for the next call would be gone before.  us with and without: 64 sequences of 16384 tokens, 8 heads (4.3 GB)
-// 625 / 710 (6.87 / 6.05 TB/s), of 4096 (1.1 GB) 161 / 185, 32 of 1024 (128 MB) 30.0 / 31.7, where they are not in that cache, of
-// 512 (64 MB) 23.8 / 24.3, but 23.4 / 21.7 where they are (three such caches in turn).
+// A call that reads more than this (by the length of its shares, what its tiles cost beside their stages among it) loads past
+// the caches (nt): as nothing of it is read twice, and what the memory-side cache (256 MB) could keep for the next call would
+// be gone before.  us with and without: 64 sequences of 16384 tokens, 8 heads (4.3 GB) 625 / 710 (6.87 / 6.05 TB/s), of 4096
+// (1.1 GB) 161 / 185, 32 of 1024 (128 MB) 30.0 / 31.7, where they are not in that cache, of 512 (64 MB) 23.8 / 24.3, but
+// 23.4 / 21.7 where they are (three such caches in turn).
 constexpr long long kFewOnce = 80ll << 20;
 constexpr int kFewItems = 8192;   // most tiles of a call whose keys are divided
 constexpr int kFewPlaces = 512;   // shares at most: places for workgroups, two a CU
