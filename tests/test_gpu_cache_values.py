@@ -7,6 +7,7 @@ import torch
 
 import paper_2605_14513_amd as heart
 from cache_reference import E4M3, Pages, near, reference
+from cache_testlib import e4m3_values
 
 pytestmark = pytest.mark.gpu
 
@@ -112,3 +113,37 @@ def test_windows_of_lengths_beyond_the_page_table(kind, D, n):
             out = heart.heart_cache_attn(q, *c.args(), causal=causal, window=window, lse=lse, workspace=workspace, **c.exps())
             near(out, want, tol, "out")
             near(lse, want_lse, ltol, "lse")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_of_few_rows_are_two_bf16(D, kind):
+    """Columns of v that the weights of all rows cancel: out is next to nothing beside sum p |v|, so what is left of a weight's
+    rounding shows.  (On the CPU: weights of one bf16 would be outside the tolerance.)"""
+    n, G = 40, 8
+    c = Pages([n], 1, D, 16, kind, seed=D)
+    q = (0.25 * new_q(1, G, D).float()).bfloat16()
+    k = c.sequence("k", 0)[0].cpu()
+    s = q[0].double().cpu() @ k.t() / math.sqrt(D)
+    p = torch.softmax(s, -1)
+    g = torch.Generator().manual_seed(2)
+    v = torch.randn((n, D), generator=g, dtype=torch.float64)
+    v = v - torch.linalg.pinv(p) @ (p @ v)
+    if kind == "e4m3":
+        v, exp = e4m3_values(v)
+        codes = torch.ldexp(v, 127 - exp.int()[:, None]).float().to(E4M3).view(torch.uint8)
+    else:
+        v = v.bfloat16().double()
+    for j in range(n):
+        page, row = place(c, 0, j)
+        if kind == "e4m3":
+            c.stored["v"].view(torch.uint8)[page, 0, row], c.exp["v"][page, 0, row] = codes[j].cuda(), exp[j].cuda()
+        else:
+            c.stored["v"][page, 0, row] = v[j].bfloat16().cuda()
+    want, _, tol, _ = reference(c, q, [1], weight=2.0**-16)
+    w = torch.exp(s - s.amax(-1, keepdim=True))
+    one = (w.float().bfloat16().double() @ v) / w.sum(-1, keepdim=True)
+    assert ((one - want[0].cpu()).abs() > tol[0].cpu()).float().mean() > 0.2
+    print(f"cache_attn weights {kind} D={D}", flush=True)
+    for workspace in ("auto", None):
+        near(heart.heart_cache_attn(q, *c.args(), workspace=workspace, **c.exps()), want, tol, "out")
