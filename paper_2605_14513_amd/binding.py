@@ -459,6 +459,10 @@ def heart_cache_read(k_cache, v_cache, page_table, kv_len, k=None, v=None, n: Op
     that the page table has room for unless it is given."""
     native = _native()
     if k is None or v is None:
+        if k_cache.dim() != 4 or page_table.dim() != 2:
+            raise ValueError("k_cache must be [n_pages,H,page,D] and page_table [B,max_pages]")
+        if any(t is not None and t.dim() != 4 for t in (k, v)):
+            raise ValueError("k and v must both be [B,H,N,D]")
         if n is None:
             n = (page_table.shape[1] * k_cache.shape[2]) if k is v else (v if k is None else k).shape[2]
         shape = (page_table.shape[0], k_cache.shape[1], n, k_cache.shape[3])
@@ -474,6 +478,8 @@ def heart_cache_read(k_cache, v_cache, page_table, kv_len, k=None, v=None, n: Op
 
 def heart_cache_attn_workspace_bytes(q, k_cache, page_table) -> int:
     """Bytes of workspace for heart_cache_attn of q [T,Hq,D] (0 where it has no use for one)."""
+    if q.dim() != 3 or k_cache.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("q must be [T,Hq,D], k_cache [n_pages,H,page,D] and page_table [B,max_pages]")
     c = HeartCache(H=k_cache.shape[1], D=k_cache.shape[3], B=page_table.shape[0])
     return int(load_library().heart_cache_attn_workspace_bytes(ctypes.byref(c), int(q.shape[0]), int(q.shape[1])))
 
