@@ -375,8 +375,8 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v| over a query's keys has to stay below 2^128.)  out
  * must not overlap q.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
- * B, H, D alone), or NULL.  With it the keys of few queries are divided over the chip, into parts that depend on all
- * lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on
+ * B, H, D alone), or NULL.  With it the keys of few queries (of at most 256 sequences) are divided over the chip, into parts
+ * that depend on all lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on
  * entry and undefined on return; two calls that run concurrently must not share one.
  */
 int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, const long long q_stride[2], const int *cu_q,

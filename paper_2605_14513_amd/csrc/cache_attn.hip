@@ -10,7 +10,10 @@
 // of two lanes, and the exponentiated accumulator is, as it is, the B operand of the second product.
 //
 // One pass with a running reference exponent, which moves only when a logit exceeds it by more than 2^8, and a running
-// sum.  The accumulators of S^T start from minus that reference.  K of slice s + 1 and V of slice s (32 keys) are worked
+// sum.  Weights are rounded to bf16 for the second product (error against 64 bits 0.0018 to 0.0020 in the 2-norm, 0.0016 of it
+// the rounding of the output): a sum of two bf16, as few rows have, would be half as many matrix instructions again where
+// these set the time.  The row sum adds the weights unrounded.
+// The accumulators of S^T start from minus that reference.  K of slice s + 1 and V of slice s (32 keys) are worked
 // on in turn: B(s) multiplies K while the VALU exponentiates slice s, C(s) multiplies V while it folds the
 // maximum of slice s + 1.
 //
@@ -25,7 +28,7 @@
 //     time than the products take.
 //
 // Bound by the matrix instructions and the power that they draw.  PFLOP/s: 4680 queries of 12 heads over 32760 keys in bf16
-// 1.03 to 1.07 (matrix pipes busy 59 % of the cycles), of 40 heads in e4m3 0.99 to 1.02 (53 %: the conversions); a bf16 matrix
+// 1.03 to 1.07 (matrix pipes busy 59 % of the cycles), of 40 heads in e4m3 0.99 to 1.04 (53 %: the conversions); a bf16 matrix
 // product of 8192^3 1.20.  Calls of few tiles are bound by latency: 16 sequences with 8 drafts of 24 heads, window 4096, 20 us.
 #include <type_traits>
 
@@ -833,8 +836,9 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   const long long items = most_items(kTile, c.B, c.H, T, Hq);
   if (items > kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   Division d = divide(c.B, items);
-  // (sequences so short that a second round of parts, and the launch that adds them up, gain nothing: causal attention of 4680 tokens
-  // to themselves, 8 heads 87 us whole, 93 divided, 16 heads 124, 129.  16 sequences of 4000 tokens and 48 queries, eight heads in
+  // (page tables with room for so few tokens, all that is known of lengths here: a second round of parts, and the launch that adds them
+  // up, gain nothing: causal attention of 4680 tokens to themselves, 8 heads 87 us whole, 93 divided, 16 heads 124, 129.  As short
+  // sequences of a table with more room are divided all the same.  16 sequences of 4000 tokens and 48 queries, eight heads in
   // e4m3: 77 whole, 44 in one round of parts)
   if (a.s.cap <= kBrief) {
     if (d.mode == kTail || (c.B == 1 && 2 * items > kPlaces)) d = {kWhole, 1, 0, 1, 0};

@@ -26,7 +26,7 @@ __device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, b);
 }
 
-constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are divided
+constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are divided: every wavefront looks at all, up to four a lane
 
 // K or V of the cache
 struct CacheTensor {

@@ -693,7 +693,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   }
 }
 
-// Rows a sequence and key head, on average, that this kernel is for: those of one tile.  us of this kernel and of the one for
+// Rows a sequence and key head, on average (all that is known of them here), that this kernel is for: those of one tile.  us, where all
+// sequences of a call are alike, of this kernel and of the one for
 // tiles of 128 rows (cache_attn.hip): 16 rows: one sequence of 2000 keys, two heads 12.6 / 16.1, of 30000, eight heads 44.6 / 47.7, 16 of
 // 4000 48.9 / 51.8, in e4m3 31.4 / 39.4, 64 of 1000 44.8 / 43.3, in e4m3 27.2 / 31.6; 24 rows (two tiles): 18 to 35 % slower
 // than that where one sequence is divided, 5 % faster to 9 % slower in batches.
