@@ -324,8 +324,8 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
  * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
  * call's tensors (NULL: each has T/B of them), and the last of them is at position kv_len[b]-1.  Tokens behind cu_q[B], and
- * output rows of them, are left alone.  cu_q must not fall and lie in [0, T]; else tokens may be left out, or taken as those of
- * another of the sequences whose ranges they are in.
+ * output rows of them, are left alone.  cu_q must not fall and lie in [0, T]; else tokens may be left out, or taken as those
+ * of any of the sequences whose ranges they are in.
  * Nothing that these arrays hold leaves the tensors: a position below 0 or from max_pages * page on is neither written nor
  * read nor seen, and a page outside [0, n_pages) is not written and reads as zeros.  Sequences may share pages that no call
  * writes; of two new tokens at one place of the cache, either or a mixture is kept.
@@ -372,12 +372,12 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values they stand for (as part
  * of the weights, v's exponents, where these are two bf16: below an exponent of 32 they lose bits).  Rows from kv_len on may
  * hold anything, pages of nobody too; a NaN or an infinity among the first kv_len tokens may also reach queries that do not see
- * it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v| over a query's keys has to stay below 2^128.)  out
- * must not overlap q.
+ * it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v| over a query's keys has to stay below 2^128, and
+ * v's exponents below 247.)  out must not overlap q.  T Hq is at most 2^30.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
  * B, H, D alone), or NULL.  With it the keys of few queries (of at most 256 sequences) are divided over the chip, into parts
- * that depend on all lengths of the call; results are those without it up to rounding, and the same for the same call.  Contents irrelevant on
- * entry and undefined on return; two calls that run concurrently must not share one.
+ * that depend on all lengths of the call; results are those without it up to rounding, and the same for the same call.
+ * Contents irrelevant on entry and undefined on return; two calls that run concurrently must not share one.
  */
 int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, const long long q_stride[2], const int *cu_q,
                      int causal, int window, float scale, void *out, const long long o_stride[2], float *lse,
