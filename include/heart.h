@@ -14,7 +14,7 @@
  *     environment variable; an entry point that needs scratch memory takes it as a
  *     workspace argument.  Workspace sizes: heart_workspace_bytes (the hot path),
  *     heart_pool_drift_workspace_bytes, heart_scores_antidiag_workspace_bytes,
- *     heart_cache_attn_workspace_bytes, heart_ebc_workspace_bytes.
+ *     heart_cache_attn_workspace_bytes, heart_cache_plan_workspace_bytes, heart_ebc_workspace_bytes.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  A call
  *     only enqueues kernels on that stream and returns; it never synchronises.
  *   - Return value: HEART_OK (0) or a negative error code.  After an error
@@ -320,6 +320,11 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  *     D: an element stands for code * 2^(exp - 127), exp 0 .. 254 (rows under 255, which are never written, may give
  *     anything).  A power of two makes reading exact (codes have 4 significant bits) and leaves one rounding, to the nearest
  *     code, in writing.
+ *   HEART_CACHE_INT8: elements are signed 8-bit whole numbers, and k_exp, v_exp point to float [n_pages,H] (contiguous,
+ *     16-byte aligned), a scale for each page and head: an element stands for code * scale.  For rows of about one size
+ *     (normalised keys) the error of writing is 2/5 of that of e4m3, for rows of very different sizes in a page it is larger.
+ *     heart_cache_write gives scales of 3 significant bits; other positive ones may be read and attended to, those of v with
+ *     up to 7 significant bits.
  * B sequences: page_table int32 [B,max_pages] names the pages of each in order, kv_len int32 [B] says how many tokens it
  * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
  * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
@@ -333,12 +338,13 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  */
 #define HEART_CACHE_BF16 0
 #define HEART_CACHE_E4M3 1
+#define HEART_CACHE_INT8 3
 typedef struct heart_cache {
   int n_pages, page, H, D, type;
   int B, max_pages;
   long long k_stride[3], v_stride[3]; /* page, head, token */
   void *k, *v;
-  unsigned char *k_exp, *v_exp;
+  unsigned char *k_exp, *v_exp; /* HEART_CACHE_INT8: float [n_pages,H] */
   const int *page_table, *kv_len;
 } heart_cache;
 
@@ -346,6 +352,11 @@ typedef struct heart_cache {
  * Writes the keys and values of the new tokens.  k, v: bf16 [T,H,D], strides {token, head} in elements (multiples of 8),
  * 16-byte aligned.  e4m3: exp is that of the smallest power of two, 2^-126 at least, under which the row's largest finite
  * element is at most 448 (127 for a row of zeros); NaN and infinities become NaN.  Nothing else of the cache is touched.
+ * int8: of the new rows of a page (and head), with a their largest magnitude: the scale s is the least m 2^e with m = 4, 5, 6, 7
+ * and 127 s >= a, at least 2^-126; 0 for a = 0; NaN, which all of the page then reads as, where one of them is NaN or infinite.
+ * A page whose first token is among the new ones gets s.  Another keeps its scale s0 if that is at least s (or NaN), else it
+ * gets s, and the codes c of the rows before the new ones become round(c s0 / s).  A new element's code is round(x / scale), ties
+ * to even.  Pages that new tokens are in must not be another sequence's too.
  */
 int heart_cache_write(const heart_cache *cache, int T, const void *k, const long long k_stride[2], const void *v,
                       const long long v_stride[2], const int *cu_q, void *stream);
@@ -383,6 +394,33 @@ int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, con
                      int causal, int window, float scale, void *out, const long long o_stride[2], float *lse,
                      void *workspace, size_t workspace_bytes, void *stream);
 size_t heart_cache_attn_workspace_bytes(const heart_cache *cache, int T, int Hq);
+
+/*
+ * Plans a step: from the requests' lengths, which pages go back and which are taken, and where each new token is written.  Its
+ * outputs are the arrays of the calls above; all is on the device, so the host need not know what was accepted or refused.
+ * Of request b, in: kv_len[b] tokens in pages page_table[b][0 ..], keep[b] (NULL: all) of them stay (clamped to 0 .. kv_len[b];
+ * 0: the request has ended, or begins anew), add[b] new ones are asked for (negative: 0).  First the pages that no kept token
+ * is in go back to the list, those of all requests; then requests are granted in order.  One is granted its add[b] tokens, all or
+ * none, if kept and new tokens fit max_pages pages, if the list has pages for it and for all before it that fit the table (or if it
+ * needs none: behind one that finds too few, only such are granted), and if the tokens of those that have their pages, up to
+ * it, are at most T.
+ * Out: kv_len[b]: kept tokens and granted ones; page_table: pages taken, -1 where one went back and none was taken, else as it
+ *   was; cu_q [B+1]: granted tokens before each request (so cu_q[b+1] - cu_q[b] says whether b was granted); slots int64 [T] or
+ *   NULL: page * page size + row of every new token, positions [T] or NULL: its position; -1 behind cu_q[B], and slots -1 in a page
+ *   outside [0, n_pages).
+ * free_pages int32 [n_pages], n_free int32 [1], in and out: the list, free_pages[0 .. n_free-1], taken from its end.  Pages go
+ *   back so that they are taken in the order in which they went back (by request, then by place in the table), before the others:
+ *   a call with the same keep and add after the first changes nothing.  Entries from n_free on are of no meaning.  A page must
+ *   be in one place only, in a table or on the list (those of kept tokens may be shared).
+ * Nothing that the arrays hold leaves them: n_free is taken as clamped to 0 .. n_pages, kv_len[b] to 0 .. max_pages * page, and
+ * pages that the list has no room for are lost.  keep may be kv_len; no other two arrays may overlap.  T <= 2^30.
+ * workspace: DEVICE, 16-byte aligned, heart_cache_plan_workspace_bytes(B, max_pages, T) bytes (0: NULL will do), contents
+ * irrelevant on entry and undefined on return; two calls that run concurrently must not share one.
+ */
+int heart_cache_plan(int B, int max_pages, int page, int n_pages, int T, const int *keep, const int *add, int *kv_len,
+                     int *page_table, int *free_pages, int *n_free, int *cu_q, long long *slots, int *positions,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t heart_cache_plan_workspace_bytes(int B, int max_pages, int T);
 
 /*
  * Error-guided Budgeted Calibration (Sec. 4.3): offline, not on the serving path.

@@ -51,7 +51,7 @@ class HeartCache(ctypes.Structure):
     ]
 
 
-HEART_CACHE_BF16, HEART_CACHE_E4M3 = 0, 1  # cache types (include/heart.h)
+HEART_CACHE_BF16, HEART_CACHE_E4M3, HEART_CACHE_INT8 = 0, 1, 3  # cache types (include/heart.h)
 
 
 def lib_path() -> str:
@@ -125,6 +125,10 @@ def load_library() -> ctypes.CDLL:
     lib.heart_cache_attn.restype = ci
     lib.heart_cache_attn_workspace_bytes.argtypes = [cp, ci, ci]
     lib.heart_cache_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.heart_cache_plan.argtypes = [ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.heart_cache_plan.restype = ci
+    lib.heart_cache_plan_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.heart_cache_plan_workspace_bytes.restype = ctypes.c_size_t
     lib.heart_last_error.restype = ctypes.c_char_p
     _lib = lib
     return lib
@@ -441,19 +445,35 @@ def heart_scores_antidiag(q, k, block: int, stride: int, scores=None, workspace=
     return scores
 
 
-def heart_cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None):
+def _units(k_cache, k_exp, v_exp, k_scale, v_scale):
+    """The exponents of a cache, or the scales of an int8 one."""
+    if k_scale is None and v_scale is None:
+        return k_exp, v_exp
+    if k_cache.dtype != torch.int8:
+        raise ValueError("k_scale, v_scale: only an int8 cache has scales")
+    if k_exp is not None or v_exp is not None:
+        raise ValueError("k_exp, v_exp: an int8 cache has scales, no exponents")
+    return k_scale, v_scale
+
+
+def heart_cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None, k_scale=None,
+                      v_scale=None):
     """Writes the keys and values of new tokens (bf16 [T,H,D]) into the pages of their sequences.
 
     k_cache, v_cache: [n_pages,H,page,D] views, bf16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages,H,page] (the rows'
-    exponents); page_table int32 [B,max_pages]; kv_len int32 [B]: tokens of each sequence, the new ones among them; cu_q
-    int32 [B+1]: where each sequence's new tokens begin (None: T/B each)."""
+    exponents), or int8 with k_scale, v_scale float32 [n_pages,H] (a scale for each page and head, which the call sets, or
+    raises where a page that has tokens gets larger ones: their codes are then divided anew); page_table int32
+    [B,max_pages]; kv_len int32 [B]: tokens of each sequence, the new ones among them; cu_q int32 [B+1]: where each sequence's
+    new tokens begin (None: T/B each)."""
+    k_exp, v_exp = _units(k_cache, k_exp, v_exp, k_scale, v_scale)
     rc = _native().cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q, k_exp, v_exp, torch._C._cuda_getDevice(),
                                _stream())
     if rc:
         _check("heart_cache_write", rc)
 
 
-def heart_cache_read(k_cache, v_cache, page_table, kv_len, k=None, v=None, n: Optional[int] = None, k_exp=None, v_exp=None):
+def heart_cache_read(k_cache, v_cache, page_table, kv_len, k=None, v=None, n: Optional[int] = None, k_exp=None, v_exp=None,
+                     k_scale=None, v_scale=None):
     """The first n cached tokens of every sequence as bf16 (k, v) [B,H,n,D], for heart_pool_qk and heart_block_sparse_attn.
     Rows behind a sequence's last token are left as they are in k and v; without k and v they are zeros, and n is all
     that the page table has room for unless it is given."""
@@ -470,6 +490,7 @@ def heart_cache_read(k_cache, v_cache, page_table, kv_len, k=None, v=None, n: Op
         v = torch.zeros(shape, dtype=torch.bfloat16, device=k_cache.device) if v is None else v
     if n is not None and n != k.shape[2]:
         raise ValueError("k must hold n tokens")
+    k_exp, v_exp = _units(k_cache, k_exp, v_exp, k_scale, v_scale)
     rc = native.cache_read(k_cache, v_cache, page_table, kv_len, k_exp, v_exp, k, v, torch._C._cuda_getDevice(), _stream())
     if rc:
         _check("heart_cache_read", rc)
@@ -485,7 +506,7 @@ def heart_cache_attn_workspace_bytes(q, k_cache, page_table) -> int:
 
 
 def heart_cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None, causal: int = 1,
-                     window: int = 0, scale: float = 0.0, out=None, lse=None, workspace="auto"):
+                     window: int = 0, scale: float = 0.0, out=None, lse=None, workspace="auto", k_scale=None, v_scale=None):
     """Attention of the new tokens' queries (bf16 [T,Hq,D]) over the cache, which holds their keys and values already (the
     cache's arguments: heart_cache_write); returns bf16 out like q (rows behind cu_q[B] are left as they are in a given out,
     and hold anything in a new one).
@@ -501,11 +522,58 @@ def heart_cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=N
         if workspace != "auto":
             raise ValueError("workspace must be a tensor, None or 'auto'")
         workspace = torch.empty(heart_cache_attn_workspace_bytes(q, k_cache, page_table), dtype=torch.uint8, device=q.device)
+    k_exp, v_exp = _units(k_cache, k_exp, v_exp, k_scale, v_scale)
     rc = native.cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q, k_exp, v_exp, causal, window, scale, out, lse,
                            workspace, torch._C._cuda_getDevice(), _stream())
     if rc:
         _check("heart_cache_attn", rc)
     return out
+
+
+def heart_cache_plan_workspace_bytes(B: int, max_pages: int, n: int) -> int:
+    """Bytes of workspace for heart_cache_plan of B requests, a page table of max_pages places each, n new tokens (0: none)."""
+    return int(load_library().heart_cache_plan_workspace_bytes(int(B), int(max_pages), int(n)))
+
+
+def heart_cache_plan(add, kv_len, page_table, free_pages, n_free, page: int, n: Optional[int] = None, keep=None, cu_q=None,
+                     slots=None, positions=None, workspace="auto"):
+    """Plans a step on the GPU: which pages go back to the list, which requests get their new tokens, their pages, and where
+    each token is written.  Returns (cu_q int32 [B+1], slots int64 [n], positions int32 [n]) for the other calls on the cache.
+
+    add int32 [B]: new tokens asked for; keep int32 [B] or None: cached tokens that stay (None: all; 0: the request has ended or
+    begins anew).  Changed in place: kv_len int32 [B] (cached tokens of each, the new ones among them at the end), page_table
+    int32 [B,max_pages], the list of free pages free_pages int32 [n_pages] with n_free int32 [1] entries.  page: tokens of a
+    page; n: new tokens there is room for (that of slots or positions where they are given).  A request gets all of its
+    tokens or, where the table, the list or n have no room for them, none: then cu_q[b+1] == cu_q[b].
+    workspace: a GPU tensor of at least heart_cache_plan_workspace_bytes bytes, None (where that is 0), or "auto" (a fresh
+    tensor from torch's allocator)."""
+    native = _native()
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B,max_pages]")
+    B, device = page_table.shape[0], page_table.device
+    for t in (slots, positions):
+        if t is not None:
+            if t.dim() != 1:
+                raise ValueError("slots and positions must be [n]")
+            if n is None:
+                n = t.shape[0]
+            elif n != t.shape[0]:
+                raise ValueError("slots and positions must hold n tokens")
+    if n is None:
+        raise ValueError("n, slots or positions must be given")
+    cu_q = torch.empty(B + 1, dtype=torch.int32, device=device) if cu_q is None else cu_q
+    slots = torch.empty(n, dtype=torch.int64, device=device) if slots is None else slots
+    positions = torch.empty(n, dtype=torch.int32, device=device) if positions is None else positions
+    if isinstance(workspace, str):
+        if workspace != "auto":
+            raise ValueError("workspace must be a tensor, None or 'auto'")
+        need = heart_cache_plan_workspace_bytes(B, page_table.shape[1], n)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    rc = native.cache_plan(add, kv_len, page_table, free_pages, n_free, page, keep, cu_q, slots, positions, workspace,
+                           torch._C._cuda_getDevice(), _stream())
+    if rc:
+        _check("heart_cache_plan", rc)
+    return cu_q, slots, positions
 
 
 def heart_ebc_workspace_bytes(C: int, T: int, Y: int, X: int) -> int:

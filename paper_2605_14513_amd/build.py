@@ -15,7 +15,7 @@ NATIVE = os.path.join(PKG, "_native.so")
 NATIVE_SOURCE = os.path.join(CSRC, "native_calls.cpp")
 SOURCES = ["heart_api.hip", "pool_qk.hip", "drift.hip", "mask_topp.hip", "attn_plan.hip",
            "block_sparse_attn.hip", "ubench.hip", "ebc.hip", "antidiag_scores.hip",
-           "cache.hip", "cache_attn.hip", "cache_attn_few.hip"]
+           "cache.hip", "cache_int8.hip", "cache_plan.hip", "cache_attn.hip", "cache_attn_few.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

@@ -10,6 +10,8 @@
 // us: reading 32760 tokens of 12 heads of 128 from e4m3 (303 MB in and out) 60 (5.1 TB/s, a copy of 512 MB 4.7), of 40 heads 189;
 // writing 4680 tokens of 40 heads and reading them back 62; the tokens of 64 sequences 4.5.  Stores past the caches make the
 // first 53, but the pooling that reads what was read back then takes 36 instead of 23.
+#include <type_traits>
+
 #include "cache_device.h"
 
 namespace heart {
@@ -138,16 +140,26 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheSide k, CacheSide
   }
 }
 
+// Two codes of w from byte kAt on, times a scale, as bf16: the product is exact where the scale has 3 significant bits, and rounded once.
+template <int kAt>
+__device__ __forceinline__ uint32_t codes_times(uint32_t w, float scale) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  const f32x2 f = {(float)(int8_t)(w >> (8 * kAt)) * scale, (float)(int8_t)(w >> (8 * kAt + 8)) * scale};
+  const bf16x2_c r = __builtin_convertvector(f, bf16x2_c);
+  return __builtin_bit_cast(uint32_t, r);
+}
+
 struct CacheOut {  // K or V
-  const uint8_t *src, *exp;
+  const uint8_t *src, *exp;  // (int8: exp is float [n_pages,H])
   long long sp, sh, st;  // page, head, token (bytes)
   uint16_t *dst;
   long long db, dh, dt;  // batch, head, token (bf16 elements)
 };
 
-template <int D, bool kCodes>
+template <int D, CacheKind kKind>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheOut k, CacheOut v, CacheSeqs s, int H, int N, int tiles) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, NI = kRowsWave / RPI;
+  constexpr bool kCodes = kKind != kBf16;
   const int lane = threadIdx.x & 63, sub = lane / LPR, col = lane % LPR;
   const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = (int)(blockIdx.x % (unsigned)tiles), bh = (int)(blockIdx.x / (unsigned)tiles);
@@ -158,18 +170,20 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheOut k, CacheOut v,
   const int page = cache_page(s, b, n0), o0 = n0 & ((1 << s.page_shift) - 1);
   u32x4_c x[2][NI];
   uint32_t byte[2][NI];
+  float scale[2];
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     const CacheOut &c = side ? v : k;
     const uint8_t *src = c.src + (long long)max(page, 0) * c.sp + h * c.sh;
-    const uint8_t *exp = kCodes ? c.exp + (((long long)max(page, 0) * H + h) << s.page_shift) : nullptr;
+    const uint8_t *exp = kKind == kE4m3 ? c.exp + (((long long)max(page, 0) * H + h) << s.page_shift) : nullptr;
+    if constexpr (kKind == kInt8) scale[side] = reinterpret_cast<const float *>(c.exp)[(long long)max(page, 0) * H + h];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int o = o0 + i * RPI + sub;
       if constexpr (kCodes) {
         const u32x2_c y = *reinterpret_cast<const u32x2_c *>(src + o * c.st + col * 8);
         x[side][i] = u32x4_c{y.x, y.y, 0, 0};
-        byte[side][i] = exp[o];
+        if constexpr (kKind == kE4m3) byte[side][i] = exp[o];
       } else {
         x[side][i] = *reinterpret_cast<const u32x4_c *>(src + o * c.st + col * 16);
       }
@@ -183,7 +197,10 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheOut k, CacheOut v,
     for (int i = 0; i < NI; ++i) {
       const int n = n0 + i * RPI + sub;
       u32x4_c y = x[side][i];
-      if constexpr (kCodes) {
+      if constexpr (kKind == kInt8) {
+        y = u32x4_c{codes_times<0>(x[side][i].x, scale[side]), codes_times<2>(x[side][i].x, scale[side]),
+                    codes_times<0>(x[side][i].y, scale[side]), codes_times<2>(x[side][i].y, scale[side])};
+      } else if constexpr (kKind == kE4m3) {
         const float unit = unit_of(byte[side][i]);
         y = u32x4_c{codes_to_bf16<false>(y.x, unit), codes_to_bf16<true>(y.x, unit), codes_to_bf16<false>(x[side][i].y, unit),
                     codes_to_bf16<true>(x[side][i].y, unit)};
@@ -196,6 +213,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheOut k, CacheOut v,
 
 int launch_cache_write(const heart_cache &c, int T, const void *k, const long long ks[2], const void *v,
                        const long long vs[2], const int *cu_q, hipStream_t st) {
+  if (c.type == HEART_CACHE_INT8) return launch_cache_write_blocks(c, T, k, ks, v, vs, cu_q, st);
   const bool codes = c.type == HEART_CACHE_E4M3;
   const long long eb = codes ? 1 : 2, waves = ((long long)T + kRowsWave - 1) / kRowsWave * c.H;
   if (waves > 4 * kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_write: too many rows (T = %d, H = %d)", T, c.H);
@@ -214,8 +232,7 @@ int launch_cache_write(const heart_cache &c, int T, const void *k, const long lo
 
 int launch_cache_read(const heart_cache &c, int N, void *k, const long long ks[3], void *v, const long long vs[3],
                       hipStream_t st) {
-  const bool codes = c.type == HEART_CACHE_E4M3;
-  const long long eb = codes ? 1 : 2, cap = (long long)c.max_pages * c.page;
+  const long long eb = c.type == HEART_CACHE_BF16 ? 2 : 1, cap = (long long)c.max_pages * c.page;
   const long long tiles = ((N < cap ? N : cap) + 4 * kRowsWave - 1) / (4 * kRowsWave);
   if ((long long)c.B * c.H > kMostGroups / tiles)
     return fail(HEART_EUNSUPPORTED, "heart_cache_read: too many rows (B = %d, H = %d, N = %d)", c.B, c.H, N);
@@ -228,8 +245,12 @@ int launch_cache_read(const heart_cache &c, int N, void *k, const long long ks[3
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * c.B * c.H)), dim3(256), 0, st, ok, ov, seqs, c.H, N, (int)tiles);
     return check_launch("cache_read_kernel");
   };
-  if (c.D == 128) return codes ? run(cache_read_kernel<128, true>) : run(cache_read_kernel<128, false>);
-  return codes ? run(cache_read_kernel<64, true>) : run(cache_read_kernel<64, false>);
+  auto of_kind = [&](auto d) -> int {
+    constexpr int D = decltype(d)::value;
+    if (c.type == HEART_CACHE_INT8) return run(cache_read_kernel<D, kInt8>);
+    return c.type == HEART_CACHE_E4M3 ? run(cache_read_kernel<D, kE4m3>) : run(cache_read_kernel<D, kBf16>);
+  };
+  return c.D == 128 ? of_kind(std::integral_constant<int, 128>{}) : of_kind(std::integral_constant<int, 64>{});
 }
 
 }  // namespace heart

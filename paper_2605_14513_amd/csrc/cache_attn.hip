@@ -157,8 +157,16 @@ __device__ __forceinline__ void item_at(const AttnCall &c, int i, int n_items, i
   }
 }
 
-template <int D, bool kCodes, CacheMode kMode>
+// (int8) Codes in a quarter of the bytes of w as f16, exactly: with the sign bit turned, the byte below 0x64 is 1024 + 128 + code.
+// Two of them, from byte 2 kUpper on: less 1152, or times `unit` less 1152 `unit` (exact for units of up to 7 significant bits).
+template <bool kUpper>
+__device__ __forceinline__ f16x2_t codes_up(uint32_t turned) {
+  return __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, turned, kUpper ? 0x04030402u : 0x04010400u));
+}
+
+template <int D, CacheKind kKind, CacheMode kMode>
 __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
+  constexpr bool kCodes = kKind != kBf16, kInts = kKind == kInt8;
   constexpr int DT = D / 32;             // 32-wide d tiles of the output
   constexpr int KS = D / 16;             // k-steps of the first product
   constexpr int CPR = D / 8;             // 16-byte chunks of a row in LDS
@@ -171,12 +179,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   constexpr int RPC = 64 / LPC;          // rows of one load
   constexpr int CPW = 16 / RPC;          // loads per wavefront and stage
   constexpr int SO = D + 8;              // LDS row stride of the output staging (elements)
-  constexpr float kRescaleSlack = 8.f;
+  // weights are at most 2^(kTop + 8), and the largest of a row is 2^kTop at least
+  constexpr float kTop = kInts ? 7.f : 0.f, kRescaleSlack = kTop + 8.f;
   constexpr float ninf = -__builtin_inff();
   const float scale_log2e = c.scale_log2e, kInitScale = 1.f / scale_log2e;
 
   // LDS: [K stage 0][K stage 1][V stage 0][V stage 1], reused for the output at the end
   extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ __align__(16) float s_unit[kInts ? 2 : 1][4];  // (int8) scales of a K stage's rows, 16 each
+  __shared__ uint32_t s_top[4];                             // (int8) V's largest scale
   const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
 
   const int t = threadIdx.x;
@@ -275,12 +286,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   // The wavefront's 16 rows of stage i (of this part) are keys key0 + 64 i + 16 wave .. of K, 32 before that of V.
   // Page ids of stages base .. base + 63, lane l that of stage base + l.
   int ids[2];
+  float units[2];  // (int8) their scales
   auto load_ids = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
     for (int is_v = 0; is_v < 2; ++is_v) {
       const int key = key0 + (base + lane) * kStage - 32 * is_v + 16 * wave;
       ids[is_v] = -1;
       if (base + lane <= n_stage && key >= 0 && key < tile_end) ids[is_v] = cache_page(c.s, wk.b, key);
+      if constexpr (kInts) {
+        const float u = reinterpret_cast<const float *>(is_v ? c.v.exp : c.k.exp)[(long long)max(ids[is_v], 0) * c.H + wk.h];
+        units[is_v] = ids[is_v] < 0 ? 0.f : u;
+      }
     }
   };
   const int in_page = (1 << c.s.page_shift) - 1;
@@ -291,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     const int id = __builtin_amdgcn_readlane(ids[is_v], i & 63);
     const int off = key & in_page;
     addr = (uint64_t)(x.p + max(id, 0) * x.page + wk.h * x.head + off * (long long)x.row);
-    if constexpr (kCodes) exp_addr = (uint64_t)(x.exp + ((((long long)max(id, 0) * c.H + wk.h) << c.s.page_shift) + off));
+    if constexpr (kKind == kE4m3) exp_addr = (uint64_t)(x.exp + ((((long long)max(id, 0) * c.H + wk.h) << c.s.page_shift) + off));
     return id < 0 ? 0 : min(tile_end - key, 16);
   };
   // LDS-direct loads (bf16): one instruction moves 16 bytes per lane to 1 KB of consecutive LDS; lane l lands at chunk
@@ -325,9 +341,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
                  "buffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0_saved) : "s"(dst), "v"(dma_off[is_v][kCodes ? 0 : ii]), "s"(dma_rs[is_v]) : "memory");
   };
-  // codes: a stage in registers, written to LDS as bf16
+  // codes: a stage in registers, written to LDS as 16-bit values
   u32x4_t raw[2][CPW];
   uint32_t raw_exp[2][CPW];
+  float raw_unit[2];  // (int8) of the wavefront's 16 rows
   const int crow = lane / LPC, cchunk = lane % LPC;
   auto load_codes = [&](int is_v, int i) __attribute__((always_inline)) {
     const uint32_t stride = is_v ? c.v.row : c.k.row;
@@ -340,13 +357,52 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     for (int ii = 0; ii < CPW; ++ii) {
       const int r = ii * RPC + crow;
       raw[is_v][ii] = __builtin_amdgcn_raw_buffer_load_b128(rs, (uint32_t)r * stride + (uint32_t)cchunk * 16u, 0, 0);
-      raw_exp[is_v][ii] = __builtin_amdgcn_raw_buffer_load_b8(es, (uint32_t)r, 0, 0);
+      if constexpr (kKind == kE4m3) raw_exp[is_v][ii] = __builtin_amdgcn_raw_buffer_load_b8(es, (uint32_t)r, 0, 0);
     }
+    if constexpr (kInts)
+      raw_unit[is_v] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(units[is_v]), i & 63));
   };
+  // (int8) V in f16 is in units of a power of two, 2^5 of which are above the largest scale of the part
+  float v_unit = 1.f, to_v_unit = 1.f;
+  if constexpr (kInts) {
+    uint32_t top = 0;
+    if (n_stage > 0) {
+      const float *scales = reinterpret_cast<const float *>(c.v.exp);
+#pragma unroll 4
+      for (int p = (key0 >> c.s.page_shift) + t; p <= (end_key - 1) >> c.s.page_shift; p += 256) {
+        const int id = cache_page(c.s, wk.b, p << c.s.page_shift);
+        const uint32_t u = __float_as_uint(scales[(long long)max(id, 0) * c.H + wk.h]);
+        top = heart_op_umax(top, id >= 0 && u < 0x7f800000u ? u : 0u);
+      }
+    }
+    top = wave_max_u32(top);
+    if (lane == 0) s_top[wave] = top;
+    __syncthreads();
+    top = heart_op_umax(heart_op_umax(s_top[0], s_top[1]), heart_op_umax(s_top[2], s_top[3]));
+    const uint32_t up = heart_op_umin(258u - (top >> 23), 253u);  // 2^(4 - exponent of the largest)
+    to_v_unit = __uint_as_float(up << 23);
+    v_unit = __uint_as_float((254u - up) << 23);
+  }
   auto store_codes = [&](int is_v, int ii, int p, int buf) __attribute__((always_inline)) {
     const int r = wave * 16 + ii * RPC + crow, f = swizzle(is_v, r);
     unsigned char *dst = smem + (2 * is_v + buf) * TILE_B + r * ROWB;
     const u32x4_t x = raw[is_v][ii];
+    if constexpr (kInts) {
+      // K as the codes are (its scales go into the logits), V times its scale
+      const _Float16 u = (_Float16)(raw_unit[1] * to_v_unit), less = (_Float16)-1152.f * u;
+      const f16x2_t u2 = {u, u}, less2 = {less, less}, less1 = {(_Float16)-1152.f, (_Float16)-1152.f};
+      u32x4_t y;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t turned = x[2 * p + w] ^ 0x80808080u;
+        const f16x2_t a = codes_up<false>(turned), b = codes_up<true>(turned);
+        y[2 * w] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(a, u2, less2) : a + less1);
+        y[2 * w + 1] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(b, u2, less2) : b + less1);
+      }
+      *reinterpret_cast<u32x4_t *>(dst + (((2 * cchunk + p) ^ f) * 16)) = y;
+      if (!is_v && ii == 0 && p == 0) s_unit[buf][wave] = raw_unit[0];
+      return;
+    }
     const float unit = unit_of(raw_exp[is_v][ii]);
     const u32x4_t y = {codes_to_bf16<false>(x[2 * p], unit), codes_to_bf16<true>(x[2 * p], unit),
                        codes_to_bf16<false>(x[2 * p + 1], unit), codes_to_bf16<true>(x[2 * p + 1], unit)};
@@ -394,6 +450,28 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const u32x4_t *>(src + ks * 16);
   }
+  // (int8) Q in f16, with its row's power of two outside: exact but for elements below 2^-32 of the row's largest
+  float row_unit = scale_log2e;  // logits in log2 units are this times K's scale times the accumulator
+  if constexpr (kInts) {
+    uint32_t top = 0, sw0, sw1;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        top = heart_op_umax(top, heart_op_umax(qf[ks].u[w] & 0x7fffu, (qf[ks].u[w] >> 16) & 0x7fffu));
+    swap_halves32(top, sw0, sw1);
+    const uint32_t up = heart_op_umin(268u - (heart_op_umax(sw0, sw1) >> 7), 253u);  // 2^(14 - exponent of the largest)
+    const float mul = __uint_as_float(up << 23);
+    row_unit = __uint_as_float((254u - up) << 23) * scale_log2e;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) qf[ks].u[w] = cvt_pk_f16(bf16lo(qf[ks].u[w]) * mul, bf16hi(qf[ks].u[w]) * mul);
+  }
+  auto mfma = [](const Frag8 &a, const Frag8 &b, const f32x16_t &acc) __attribute__((always_inline)) {
+    if constexpr (kInts) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.h, b.h, acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, acc, 0, 0, 0);
+  };
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -447,7 +525,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
       xt1 = __builtin_amdgcn_exp2f(x[r + 1]);
       asm volatile("" : "+v"(xt1));
     } else {
-      uint32_t pk = cvt_pk_bf16(xt0, xt1);
+      uint32_t pk = kInts ? cvt_pk_f16(xt0, xt1) : cvt_pk_bf16(xt0, xt1);
       l_run += xt0 + xt1;
       asm volatile("" : "+v"(pk), "+v"(l_run));
       pf[r / 8].u[(r % 8) / 2] = pk;
@@ -455,12 +533,31 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   };
   constexpr int UB = 16 / KS;  // micro-ops of a B slot
   constexpr int UC = 8 / DT;   // micro-ops of a C slot m < DT
+  // (int8) what turns accumulators of the slice of position g into logits relative to the reference: factors of its two
+  // groups of 16 keys (no smaller than a normal number, so that -inf stays -inf), and the reference
+  float factor[2], less = 0.f;
+  auto load_factors = [&](int g) __attribute__((always_inline)) {
+    if constexpr (kInts) {
+      const int n = g / STEP + 1;
+      const f32x2_t u = *reinterpret_cast<const f32x2_t *>(&s_unit[(n >> 1) & 1][(n & 1) * 2]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float x = u[i] * row_unit;
+        factor[i] = x < 1.17549435e-38f ? 1.17549435e-38f : x;
+      }
+    }
+  };
+  auto to_logit = [&](float x, int r) __attribute__((always_inline)) -> float {
+    if constexpr (kInts) return fmaf(x, factor[r / 8], less);
+    else return x * scale_log2e;
+  };
   auto qk_step = [&](int dst, int g0, auto &&extra) __attribute__((always_inline)) {
     f32x16_t acc;
     const f32x16_t &prev = sacc[dst ^ 1];
+    load_factors(g0);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(g0 + ks) % PF].v, qf[ks].v, ks == 0 ? cinit : acc, 0, 0, 0);
+      acc = mfma(ring[(g0 + ks) % PF], qf[ks], ks == 0 ? cinit : acc);
       prefetch_after(g0 + ks);
 #pragma unroll
       for (int u = 0; u < UB; ++u) exp_uop(prev, ks * UB + u);
@@ -494,8 +591,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
       m_rel = fmaxf(__uint_as_float(sw0), __uint_as_float(sw1));
       const bool bump = m_rel > kRescaleSlack || (first && m_rel > ninf);
       const float base = first ? 0.f : m_ref;
-      const float delta = bump ? m_rel : 0.f;
-      const float m_new = bump ? base + m_rel : m_ref;
+      const float delta = bump ? m_rel - kTop : 0.f;
+      const float m_new = bump ? base + (m_rel - kTop) : m_ref;
       const float alpha = bump ? __builtin_amdgcn_exp2f(m_ref - m_new) : 1.f;  // 0 the first time
       l_run *= alpha;
 #pragma unroll
@@ -505,9 +602,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] -= delta;
       m_ref = m_new;
-      const float c0 = m_ref == ninf ? 0.f : -m_ref * kInitScale;
+      if constexpr (kInts) {
+        less = m_ref == ninf ? 0.f : -m_ref;
+      } else {
+        const float c0 = m_ref == ninf ? 0.f : -m_ref * kInitScale;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) cinit[r] = c0;
+        for (int r = 0; r < 16; ++r) cinit[r] = c0;
+      }
     }
   };
   // O^T += V^T P^T of the slice in sacc[cur]; the second half of the slots scales sacc[cur ^ 1] to log2 units and folds
@@ -518,7 +619,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     const f32x16_t &cx = sacc[cur];
 #pragma unroll
     for (int m = 0; m < NPV; ++m) {
-      o[m % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(g0 + m) % PF].v, pf[m / DT].v, o[m % DT], 0, 0, 0);
+      o[m % DT] = mfma(ring[(g0 + m) % PF], pf[m / DT], o[m % DT]);
       prefetch_after(g0 + m);
       if (m < DT) {
 #pragma unroll
@@ -529,7 +630,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
         for (int i = 0; i < 4 / DT; ++i) {
           const int p = (m - DT) * (4 / DT) + i;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) nx[4 * p + e] *= scale_log2e;
+          for (int e = 0; e < 4; ++e) nx[4 * p + e] = to_logit(nx[4 * p + e], 4 * p + e);
           m_loc = max_part(nx, p, m_loc);
         }
       }
@@ -557,10 +658,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
         for (int ks = 0; ks < KS; ++ks) {
           Frag8 a;
           a.u = fetch(3 * STEP + ks);  // K of slice 0: buffer 0, rows 0
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, qf[ks].v, acc, 0, 0, 0);
+          acc = mfma(a, qf[ks], acc);
         }
+        load_factors(3 * STEP);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] *= scale_log2e;
+        for (int r = 0; r < 16; ++r) acc[r] = to_logit(acc[r], r);
         sacc[0] = acc;
         mask_slice(sacc[0], 0);
         float m_loc = ninf;
@@ -618,7 +720,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        o4[(4 * dt + g) * 64 + lane] = f32x4_t{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+        o4[(4 * dt + g) * 64 + lane] = f32x4_t{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]} * v_unit;
     return;
   }
 
@@ -635,8 +737,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       u32x2_t pk;
-      pk.x = cvt_pk_bf16(o[dt][4 * g + 0] * inv, o[dt][4 * g + 1] * inv);
-      pk.y = cvt_pk_bf16(o[dt][4 * g + 2] * inv, o[dt][4 * g + 3] * inv);
+      pk.x = cvt_pk_bf16(o[dt][4 * g + 0] * inv * v_unit, o[dt][4 * g + 1] * inv * v_unit);
+      pk.y = cvt_pk_bf16(o[dt][4 * g + 2] * inv * v_unit, o[dt][4 * g + 3] * inv * v_unit);
       *reinterpret_cast<u32x2_t *>(sO + (wave * 32 + l32) * SO + dt * 32 + 8 * g + 4 * hf) = pk;
     }
   __syncthreads();
@@ -791,13 +893,13 @@ size_t cache_attn_workspace_bytes(int B, int H, int D, int T, int Hq) {
   return d.mode == kWhole ? 0 : kPlaces * sizeof(int4) + (size_t)d.slots() * 4 * part * sizeof(float);
 }
 
-template <int D, bool kCodes>
+template <int D, CacheKind kKind>
 static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
   constexpr int lds = 4 * kStage * D * 2, staging = kTile * (D + 8) * 2, bytes = lds > staging ? lds : staging;
   auto run = [&](auto mode, long long grid) -> int {
-    auto kern = cache_attn_kernel<D, kCodes, decltype(mode)::value>;
+    auto kern = cache_attn_kernel<D, kKind, decltype(mode)::value>;
     static DeviceFlags attr_set;  // per instantiation: the attribute is per function and device
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
       return fail(HEART_EHIP, "hipFuncSetAttribute(max dynamic LDS %d): %s", bytes, hipGetErrorString(e));
@@ -820,8 +922,7 @@ static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
 int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const long long qs[2], const int *cu_q, int causal,
                       int window, float scale, void *out, const long long os[2], float *lse, void *workspace,
                       hipStream_t st) {
-  const bool codes = c.type == HEART_CACHE_E4M3;
-  const long long eb = codes ? 1 : 2;
+  const long long eb = c.type == HEART_CACHE_BF16 ? 2 : 1;
   AttnCall a{};
   a.k = CacheTensor{(const uint8_t *)c.k, c.k_exp, c.k_stride[0] * eb, c.k_stride[1] * eb, (uint32_t)(c.k_stride[2] * eb)};
   a.v = CacheTensor{(const uint8_t *)c.v, c.v_exp, c.v_stride[0] * eb, c.v_stride[1] * eb, (uint32_t)(c.v_stride[2] * eb)};
@@ -851,8 +952,12 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   a.tail = d.tail;
   a.items = (int4 *)workspace;
   a.part = workspace ? (float *)(a.items + kPlaces) : nullptr;
-  if (c.D == 128) return codes ? launch_t<128, true>(a, d, st) : launch_t<128, false>(a, d, st);
-  return codes ? launch_t<64, true>(a, d, st) : launch_t<64, false>(a, d, st);
+  auto of_kind = [&](auto dim) -> int {
+    constexpr int D = decltype(dim)::value;
+    if (c.type == HEART_CACHE_INT8) return launch_t<D, kInt8>(a, d, st);
+    return c.type == HEART_CACHE_E4M3 ? launch_t<D, kE4m3>(a, d, st) : launch_t<D, kBf16>(a, d, st);
+  };
+  return c.D == 128 ? of_kind(std::integral_constant<int, 128>{}) : of_kind(std::integral_constant<int, 64>{});
 }
 
 }  // namespace heart

@@ -14,10 +14,13 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 
 union Frag8 {
   u32x4_t u;
   bf16x8_t v;
+  f16x8_t h;
 };
 
 __device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
@@ -26,11 +29,17 @@ __device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, b);
 }
 
+__device__ __forceinline__ uint32_t cvt_pk_f16(float lo, float hi) {
+  f32x2_t f = {lo, hi};
+  f16x2_t b = __builtin_convertvector(f, f16x2_t);
+  return __builtin_bit_cast(uint32_t, b);
+}
+
 constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are divided: every wavefront looks at all, up to four a lane
 
 // K or V of the cache
 struct CacheTensor {
-  const uint8_t *p, *exp;
+  const uint8_t *p, *exp;  // (int8: exp is float [n_pages,H])
   long long page, head;  // bytes
   uint32_t row;          // bytes between tokens
 };

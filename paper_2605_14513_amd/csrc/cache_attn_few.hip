@@ -113,8 +113,9 @@ struct Shares {
   }
 };
 
-template <int D, bool kCodes>
+template <int D, CacheKind kKind>
 struct FewShape {
+  static constexpr bool kCodes = kKind != kBf16;
   static constexpr int ROWB = kCodes ? D : 2 * D;        // bytes of a row
   static constexpr int SK = 4096 / ROWB;                 // keys of a slice
   static constexpr int NT = SK / 16;                     // key tiles of 16
@@ -124,10 +125,19 @@ struct FewShape {
   static constexpr int NI = 16 * ROWB / 1024;            // LDS-direct loads of 16 rows
 };
 
+// (int8) Four codes as bf16, which has room for them: fp32 cut to its upper half.
+__device__ __forceinline__ u32x2_t ints_to_bf16(uint32_t w) {
+  uint32_t f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __float_as_uint((float)(int8_t)(w >> (8 * i)));
+  return u32x2_t{__builtin_amdgcn_perm(f[1], f[0], 0x07060302u), __builtin_amdgcn_perm(f[3], f[2], 0x07060302u)};
+}
+
 // SEQS: sequences a lane where the keys are divided, 0 = they are not
-template <int D, bool kCodes, int SEQS>
+template <int D, CacheKind kKind, int SEQS>
 __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c) {
-  using F = FewShape<D, kCodes>;
+  using F = FewShape<D, kKind>;
+  constexpr bool kCodes = F::kCodes, kInts = kKind == kInt8;
   constexpr bool kSplit = SEQS > 0;
   constexpr int TILE = kFewTile, ROWB = F::ROWB, SK = F::SK, NT = F::NT, NI = F::NI;
   constexpr int NC = ROWB / 16, RPB = 256 / ROWB, RPI = 1024 / ROWB;  // chunks of a row, rows per 256 bytes, rows of a load
@@ -338,10 +348,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
       }
     }
   };
-  // (codes) exponents of slice i, 4 bytes a lane: K of its tiles, then V; pages that are none: of page 0
+  // (codes) exponents of slice i, 4 bytes a lane: K of its tiles, then V; pages that are none: of page 0.  Of int8 the scales, one a tile.
   auto bring_exps = [&](int i, int ahead) __attribute__((always_inline)) {
     if constexpr (kCodes) {
-      const int dw = lane % (8 * NT), n = (dw >> 2) % NT;
+      const int dw = lane % (kInts ? 2 * NT : 8 * NT), n = (kInts ? dw : dw >> 2) % NT;
       int id = -1;
 #pragma unroll
       for (int m = 0; m < NT; ++m) {
@@ -351,8 +361,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
       }
       id = max(id, 0);
       const int key = key0 + i * (4 * SK) + 16 * n;
-      const uint8_t *base = dw >= 4 * NT ? c.v.exp : c.k.exp;
-      const uint8_t *addr = base + ((((long long)id * c.H + head) << c.s.page_shift) + (key & in_page) + 4 * (dw & 3));
+      const uint8_t *base = dw >= (kInts ? NT : 4 * NT) ? c.v.exp : c.k.exp;
+      const uint8_t *addr = kInts ? base + ((long long)id * c.H + head) * 4
+                                  : base + ((((long long)id * c.H + head) << c.s.page_shift) + (key & in_page) + 4 * (dw & 3));
       const uint32_t dst = wave_lds + (uint32_t)((i & 1) * F::SLICE_B + 2 * F::TENSOR_B);
       uint32_t m0_saved;
       asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
@@ -365,6 +376,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   Frag8 qf[KS];
   f32x4_t o[DT];
   float m_ref = ninf, c0 = 0.f, l_run = 0.f;  // reference exponent, minus that in raw logits, this lane's part of the row sum
+  float less = 0.f;  // (int8) minus the reference exponent, where there is one
   {
     const Row at = at0.row(head, min(l16, n_rows - 1));
     const uint16_t *src = c.q + at.token * c.qt + at.head * c.qh;
@@ -391,10 +403,26 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
       const int key = key0 + i * (4 * SK);
       // ---- S^T ------------------------------------------------------------------------------
       Frag8 kf[NT][KS];
-      float vu[NT][4];  // (codes) powers of two of V's rows 16 n + 4 g + 0..3
+      float vu[NT][4];  // (codes) powers of two of V's rows 16 n + 4 g + 0..3, or their scale
+      float factor[NT];  // of the logits
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        if constexpr (kCodes) {
+        factor[n] = scale_log2e;
+        if constexpr (kInts) {
+          const uint32_t *units = reinterpret_cast<const uint32_t *>(se);
+          factor[n] *= __uint_as_float(units[n] & named[0][n]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vu[n][e] = __uint_as_float(units[NT + n] & named[0][n]);
+#pragma unroll
+          for (int j = 0; j < KR; ++j) {
+            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(sk + 16 * n * ROWB + koff[j]);
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const u32x2_t a = ints_to_bf16(x[2 * p]), b = ints_to_bf16(x[2 * p + 1]);
+              kf[n][2 * j + p].u = u32x4_t{a.x, a.y, b.x, b.y};
+            }
+          }
+        } else if constexpr (kCodes) {
           // (a page that is none has exponents of another: 0, so that its zeros stay zeros)
           const float ku = unit_of(min((uint32_t)se[16 * n + l16] & named[0][n], 254u));
           const uint32_t ve = *reinterpret_cast<const uint32_t *>(se + 16 * NT + 16 * n + 4 * g) & named[0][n];
@@ -424,7 +452,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
         f32x4_t acc = {c0, c0, c0, c0};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][ks].v, qf[ks].v, acc, 0, 0, 0);
-        x[n] = acc * scale_log2e;
+        if constexpr (kInts) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[n][e] = fmaf(acc[e], factor[n], less);
+        } else {
+          x[n] = acc * scale_log2e;
+        }
       }
       if (key < all_lo || key + SK > all_hi) {
 #pragma unroll
@@ -455,7 +488,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
 #pragma unroll
         for (int n = 0; n < NT; ++n) x[n] -= delta;
         m_ref = m_new;
-        c0 = m_new == ninf ? 0.f : -m_new * inv_scale;
+        if constexpr (kInts) less = m_new == ninf ? 0.f : -m_new;
+        else c0 = m_new == ninf ? 0.f : -m_new * inv_scale;
       }
       // ---- weights ------------------------------------------------------------------------------
       // (as a sum of two bf16: the weights of few rows can have 16 bits where reading the cache is what takes the time)
@@ -489,6 +523,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
             Frag8 a;
             if constexpr (kCodes) {
               const i32x2_t r = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at));
+              if constexpr (kInts) {
+                const u32x2_t y0 = ints_to_bf16((uint32_t)r.x), y1 = ints_to_bf16((uint32_t)r.y);
+                a.u = u32x4_t{y0.x, y0.y, y1.x, y1.y};
+              } else
               a.u = u32x4_t{codes_to_bf16<false>((uint32_t)r.x, 1.f), codes_to_bf16<true>((uint32_t)r.x, 1.f),
                             codes_to_bf16<false>((uint32_t)r.y, 1.f), codes_to_bf16<true>((uint32_t)r.y, 1.f)};
             } else {
@@ -706,14 +744,14 @@ size_t cache_attn_few_workspace_bytes(int B, int H, int D, int T, int Hq) {
   return 2 * (size_t)kFewPlaces * (sizeof(unsigned long long) + (size_t)(kFewTile * (D + 2)) * sizeof(float));
 }
 
-template <int D, bool kCodes>
+template <int D, CacheKind kKind>
 static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
-  constexpr int bytes = 4 * FewShape<D, kCodes>::WAVE_B;
+  constexpr int bytes = 4 * FewShape<D, kKind>::WAVE_B;
   static_assert(bytes >= (256 / (D / 8)) * (D + 2) * 4, "sums of the parts fit the LDS");
   auto run = [&](auto seqs) -> int {
-    auto kern = cache_attn_few_kernel<D, kCodes, decltype(seqs)::value>;
+    auto kern = cache_attn_few_kernel<D, kKind, decltype(seqs)::value>;
     static DeviceFlags attr_set;  // per instantiation: the attribute is per function and device
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
       return fail(HEART_EHIP, "hipFuncSetAttribute(max dynamic LDS %d): %s", bytes, hipGetErrorString(e));
@@ -725,7 +763,6 @@ static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream
 }
 
 int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, void *workspace, hipStream_t st) {
-  const bool codes = hc.type == HEART_CACHE_E4M3;
   const long long items = most_items(kFewTile, hc.B, hc.H, T, Hq);
   if (items > kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   const long long stages = ((long long)a.s.cap + kFewStage - 1) / kFewStage;
@@ -738,8 +775,12 @@ int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, voi
     a.part = (float *)(a.flags + 2 * kFewPlaces);
     a.mark = call_mark();
   }
-  if (hc.D == 128) return codes ? launch_few_t<128, true>(a, split, grid, st) : launch_few_t<128, false>(a, split, grid, st);
-  return codes ? launch_few_t<64, true>(a, split, grid, st) : launch_few_t<64, false>(a, split, grid, st);
+  auto of_kind = [&](auto d) -> int {
+    constexpr int D = decltype(d)::value;
+    if (hc.type == HEART_CACHE_INT8) return launch_few_t<D, kInt8>(a, split, grid, st);
+    return hc.type == HEART_CACHE_E4M3 ? launch_few_t<D, kE4m3>(a, split, grid, st) : launch_few_t<D, kBf16>(a, split, grid, st);
+  };
+  return hc.D == 128 ? of_kind(std::integral_constant<int, 128>{}) : of_kind(std::integral_constant<int, 64>{});
 }
 
 }  // namespace heart

@@ -30,6 +30,9 @@ __device__ __forceinline__ int cache_page(const CacheSeqs &s, int b, int pos) {
   return (unsigned)id < (unsigned)s.n_pages ? id : -1;
 }
 
+// What a cache's elements are (heart_cache's type).
+enum CacheKind { kBf16 = HEART_CACHE_BF16, kE4m3 = HEART_CACHE_E4M3, kInt8 = HEART_CACHE_INT8 };
+
 // Two codes (the lower or the upper half of w) as bf16 times a power of two: exact.
 template <bool kUpper>
 __device__ __forceinline__ uint32_t codes_to_bf16(uint32_t w, float unit) {

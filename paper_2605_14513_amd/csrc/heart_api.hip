@@ -319,15 +319,15 @@ static int check_cache(const heart_cache *c, const char *fn) {
   if (c->D != 64 && c->D != 128) return fail(HEART_EUNSUPPORTED, "%s: D must be 64 or 128 (got %d)", fn, c->D);
   if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)) != 0)
     return fail(HEART_EUNSUPPORTED, "%s: page must be 16, 32, 64, 128 or 256 (got %d)", fn, c->page);
-  if (c->type != HEART_CACHE_BF16 && c->type != HEART_CACHE_E4M3)
+  if (c->type != HEART_CACHE_BF16 && c->type != HEART_CACHE_E4M3 && c->type != HEART_CACHE_INT8)
     return fail(HEART_EINVAL, "%s: unknown cache type %d", fn, c->type);
-  const bool e4m3 = c->type == HEART_CACHE_E4M3;
-  if (!c->k || !c->v || !c->page_table || !c->kv_len || (e4m3 && (!c->k_exp || !c->v_exp)))
+  const bool codes = c->type != HEART_CACHE_BF16;
+  if (!c->k || !c->v || !c->page_table || !c->kv_len || (codes && (!c->k_exp || !c->v_exp)))
     return fail(HEART_EINVAL, "%s: NULL pointer in the cache", fn);
-  if (!e4m3 && (c->k_exp || c->v_exp)) return fail(HEART_EINVAL, "%s: a bf16 cache has no exponents", fn);
+  if (!codes && (c->k_exp || c->v_exp)) return fail(HEART_EINVAL, "%s: a bf16 cache has no exponents", fn);
   if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_exp) || !aligned16(c->v_exp))
     return fail(HEART_EUNSUPPORTED, "%s: the cache must be 16-byte aligned", fn);
-  const int step = e4m3 ? 16 : 8;
+  const int step = codes ? 16 : 8;
   for (const long long *s : {c->k_stride, c->v_stride}) {
     if (s[0] % step != 0 || s[1] % step != 0 || s[2] % step != 0 || s[2] <= 0)
       return fail(HEART_EUNSUPPORTED, "%s: cache strides must be multiples of 16 bytes, token strides > 0", fn);
@@ -417,6 +417,36 @@ int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, con
 size_t heart_cache_attn_workspace_bytes(const heart_cache *c, int T, int Hq) {
   if (!c || c->B <= 0 || c->H <= 0 || (c->D != 64 && c->D != 128) || T <= 0 || Hq <= 0 || Hq % c->H != 0) return 0;
   return cache_attn_workspace_bytes(c->B, c->H, c->D, T, Hq);
+}
+
+size_t heart_cache_plan_workspace_bytes(int B, int max_pages, int T) {
+  if (B <= 0 || max_pages <= 0 || T < 0) return 0;
+  return cache_plan_workspace_bytes(B, max_pages, T);
+}
+
+int heart_cache_plan(int B, int max_pages, int page, int n_pages, int T, const int *keep, const int *add, int *kv_len,
+                     int *page_table, int *free_pages, int *n_free, int *cu_q, long long *slots, int *positions,
+                     void *workspace, size_t workspace_bytes, void *stream) {
+  clear_error();
+  const char *fn = "heart_cache_plan";
+  if (B <= 0 || max_pages <= 0 || n_pages <= 0)
+    return fail(HEART_EINVAL, "%s: B, max_pages, n_pages must be positive (got %d, %d, %d)", fn, B, max_pages, n_pages);
+  if (page < 16 || page > 256 || (page & (page - 1)) != 0)
+    return fail(HEART_EUNSUPPORTED, "%s: page must be 16, 32, 64, 128 or 256 (got %d)", fn, page);
+  if (max_pages > 0x7fffffff / page) return fail(HEART_EUNSUPPORTED, "%s: max_pages * page must stay below 2^31", fn);
+  if (T < 0) return fail(HEART_EINVAL, "%s: T must not be negative (got %d)", fn, T);
+  if (T > (1 << 30) || B > (1 << 30))
+    return fail(HEART_EUNSUPPORTED, "%s: T and B must not exceed 2^30 (got %d, %d)", fn, T, B);
+  if (!add || !kv_len || !page_table || !free_pages || !n_free || !cu_q)
+    return fail(HEART_EINVAL, "%s: NULL pointer argument", fn);
+  const size_t need = heart_cache_plan_workspace_bytes(B, max_pages, T);
+  if (need) {
+    if (!workspace || workspace_bytes < need)
+      return fail(HEART_EINVAL, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned16(workspace)) return fail(HEART_EUNSUPPORTED, "%s: workspace must be 16-byte aligned", fn);
+  }
+  return launch_cache_plan(B, max_pages, page, n_pages, T, keep, add, kv_len, page_table, free_pages, n_free, cu_q, slots,
+                           positions, workspace, (hipStream_t)stream);
 }
 
 int heart_ebc_band_error(long long C, int T, int Y, int X, const float *err, const float *dense,

@@ -28,6 +28,8 @@ const char *torch_name(at::ScalarType t) {
     case at::kFloat: return "torch.float32";
     case at::kDouble: return "torch.float64";
     case at::kInt: return "torch.int32";
+    case at::kLong: return "torch.int64";
+    case at::kChar: return "torch.int8";
     case at::kByte: return "torch.uint8";
     case at::kFloat8_e4m3fn: return "torch.float8_e4m3fn";
     default: return c10::toString(t);
@@ -289,13 +291,13 @@ void outer_strides(const Tensor &t, const char *name, int n, long long *out) {
   if (t.stride(n) != 1) value_error(std::string(name) + " must have a contiguous D axis");
   for (int i = 0; i < n; ++i) out[i] = t.size(i) == 1 ? 0 : t.stride(i);
 }
-// k_cache, v_cache, page_table, kv_len; k_exp, v_exp
+// k_cache, v_cache, page_table, kv_len; k_exp, v_exp (of int8 caches the scales)
 heart_cache cache_of(PyObject *const *a, PyObject *const *exps, long device) {
   const Tensor &k = on(a[0], "k_cache", device), &v = on(a[1], "v_cache", device), &table = on(a[2], "page_table", device);
   if (k.dim() != 4 || v.sizes() != k.sizes()) value_error("k_cache and v_cache must both be [n_pages,H,page,D]");
   const at::ScalarType type = k.scalar_type();
-  if (type != at::kBFloat16 && type != at::kFloat8_e4m3fn)
-    type_error(std::string("k_cache must have dtype torch.bfloat16 or torch.float8_e4m3fn, got ") + torch_name(type));
+  if (type != at::kBFloat16 && type != at::kFloat8_e4m3fn && type != at::kChar)
+    type_error(std::string("k_cache must have dtype torch.bfloat16 or torch.float8_e4m3fn or torch.int8, got ") + torch_name(type));
   check_type(v, type, "v_cache");
   if (table.dim() != 2) value_error("page_table must be [B,max_pages]");
   for (int i = 0; i < 4; ++i)
@@ -303,7 +305,7 @@ heart_cache cache_of(PyObject *const *a, PyObject *const *exps, long device) {
   if (table.size(0) > INT_MAX || table.size(1) > INT_MAX) value_error("page_table is too large");
   heart_cache c{};
   c.n_pages = (int)k.size(0), c.H = (int)k.size(1), c.page = (int)k.size(2), c.D = (int)k.size(3);
-  c.type = type == at::kBFloat16 ? HEART_CACHE_BF16 : HEART_CACHE_E4M3;
+  c.type = type == at::kBFloat16 ? HEART_CACHE_BF16 : type == at::kChar ? HEART_CACHE_INT8 : HEART_CACHE_E4M3;
   c.B = (int)table.size(0), c.max_pages = (int)table.size(1);
   outer_strides(k, "k_cache", 3, c.k_stride);
   outer_strides(v, "v_cache", 3, c.v_stride);
@@ -311,16 +313,18 @@ heart_cache cache_of(PyObject *const *a, PyObject *const *exps, long device) {
   c.page_table = ints(a[2], "page_table", device, table.sizes(), "");
   const int64_t lens[1] = {c.B};
   c.kv_len = ints(a[3], "kv_len", device, lens, "kv_len must be [B]");
-  const char *names[2] = {"k_exp", "v_exp"};
+  const bool blocks = c.type == HEART_CACHE_INT8;
+  const char *names[2] = {blocks ? "k_scale" : "k_exp", blocks ? "v_scale" : "v_exp"};
   unsigned char **to[2] = {&c.k_exp, &c.v_exp};
   for (int i = 0; i < 2; ++i) {
     if (c.type == HEART_CACHE_BF16) {
-      if (exps[i] != Py_None) value_error(std::string(names[i]) + ": a bf16 cache has no exponents");
+      if (exps[i] != Py_None) value_error(std::string(names[i]) + ": a bf16 cache has no exponents and no scales");
       continue;
     }
     const Tensor &e = on(exps[i], names[i], device);
-    check_type(e, at::kByte, names[i]);
-    if (e.sizes() != k.sizes().slice(0, 3)) value_error(std::string(names[i]) + " must be [n_pages,H,page]");
+    check_type(e, blocks ? at::kFloat : at::kByte, names[i]);
+    if (e.sizes() != k.sizes().slice(0, blocks ? 2 : 3))
+      value_error(std::string(names[i]) + (blocks ? " must be [n_pages,H]" : " must be [n_pages,H,page]"));
     if (!e.is_contiguous()) value_error(std::string(names[i]) + " must be contiguous");
     *to[i] = static_cast<unsigned char *>(e.data_ptr());
   }
@@ -411,6 +415,51 @@ PyObject *cache_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// contiguous tensor of the device, of a type and `n` axes
+const Tensor &array(PyObject *o, const char *name, long device, at::ScalarType type, int n, const char *msg) {
+  const Tensor &t = on(o, name, device);
+  check_type(t, type, name);
+  if (t.dim() != n) value_error(msg);
+  for (int i = 0; i < n; ++i)
+    if (t.size(i) > INT_MAX) value_error(std::string(name) + " is too large");
+  if (!t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+  return t;
+}
+
+PyObject *cache_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  check_count(n, 13);
+  const long device = integer(a[11]);
+  const Tensor &table = array(a[2], "page_table", device, at::kInt, 2, "page_table must be [B,max_pages]");
+  const int B = (int)table.size(0), M = (int)table.size(1);
+  const int64_t each[1] = {B}, ends[1] = {(int64_t)B + 1}, one[1] = {1};
+  const int *add = ints(a[0], "add", device, each, "add must be [B]");
+  int *kv_len = const_cast<int *>(ints(a[1], "kv_len", device, each, "kv_len must be [B]"));
+  const Tensor &list = array(a[3], "free_pages", device, at::kInt, 1, "free_pages must be [n_pages]");
+  int *n_free = const_cast<int *>(ints(a[4], "n_free", device, one, "n_free must be [1]"));
+  const int page = whole32(a[5], "page");
+  const int *keep = a[6] == Py_None ? nullptr : ints(a[6], "keep", device, each, "keep must be [B]");
+  int *cu = const_cast<int *>(ints(a[7], "cu_q", device, ends, "cu_q must be [B+1]"));
+  const Tensor &slots = array(a[8], "slots", device, at::kLong, 1, "slots must be [T]");
+  const Tensor &positions = array(a[9], "positions", device, at::kInt, 1, "positions must be [T]");
+  if (slots.size(0) != positions.size(0)) value_error("slots and positions must have the same shape");
+  size_t ws_bytes = 0;
+  void *ws = nullptr;
+  if (a[10] != Py_None) {
+    on(a[10], "workspace", device);
+    ws = scratch(a[10], &ws_bytes);
+  }
+  int *tp = static_cast<int *>(table.data_ptr()), *lp = static_cast<int *>(list.data_ptr()),
+      *pp = static_cast<int *>(positions.data_ptr());
+  long long *sp = static_cast<long long *>(slots.data_ptr());
+  const int n_pages = (int)list.size(0), T = (int)slots.size(0);
+  void *st = handle(a[12]);
+  return call([&] {
+    return heart_cache_plan(B, M, page, n_pages, T, keep, add, kv_len, tp, lp, n_free, cu, sp, pp, ws, ws_bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject *ebc_band_error(PyObject *, PyObject *const *a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   check_count(n, 10);
@@ -447,6 +496,7 @@ PyMethodDef methods[] = {
     {"ebc_band_error", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(ebc_band_error)), METH_FASTCALL, nullptr},
     {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_write)), METH_FASTCALL, nullptr},
     {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, nullptr},
+    {"cache_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_plan)), METH_FASTCALL, nullptr},
     {"cache_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attn)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", HEART_TORCH, -1, methods, nullptr, nullptr, nullptr, nullptr};
