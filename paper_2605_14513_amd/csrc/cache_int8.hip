@@ -63,6 +63,9 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
 }
 
 // WAVES wavefronts for a job, a workgroup of 256 threads for 4 / WAVES jobs.
+#ifndef W64
+#define W64 4
+#endif
 template <int D, int PAGE, int WAVES>
 __global__ __launch_bounds__(256) void cache_write_blocks_kernel(BlockSide k, BlockSide v, CacheSeqs s, int H, long long n_jobs) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, ROWS = PAGE / WAVES, NI = ROWS / RPI;  // lanes of a row, rows of a load and a wavefront
@@ -85,10 +88,8 @@ __global__ __launch_bounds__(256) void cache_write_blocks_kernel(BlockSide k, Bl
   const long long lo = ((p_lo >> s.page_shift) + m) << s.page_shift;  // position of the page's first token
   if (m < 0 || lo >= p_hi) return;
   const int page = cache_page(s, b, (int)lo);
-  if (page < 0) return;
   const int o0 = (int)max(p_lo - lo, 0ll), o1 = (int)min(p_hi - lo, (long long)PAGE);  // rows of the page that are new
   const uint16_t *src = c.src + (first + (lo - pos0)) * c.st + h * c.sh + col * 8;
-  float *scale_at = c.scale + ((long long)page * H + h);
   const int r0 = WAVES > 1 ? wave % WAVES * ROWS : 0;
   u32x4_c x[NI];
   uint32_t top = 0;
@@ -98,6 +99,8 @@ __global__ __launch_bounds__(256) void cache_write_blocks_kernel(BlockSide k, Bl
     x[i] = u32x4_c{0, 0, 0, 0};
     if (r >= o0 && r < o1) x[i] = *reinterpret_cast<const u32x4_c *>(src + r * c.st);
   }
+  if (page < 0) return;  // (here, so that rows are on their way meanwhile)
+  float *scale_at = c.scale + ((long long)page * H + h);
   const float had = o0 > 0 ? *scale_at : 0.f;
 #pragma unroll
   for (int i = 0; i < NI; ++i)
@@ -166,7 +169,7 @@ int launch_cache_write_blocks(const heart_cache &c, int T, const void *k, const 
     switch (c.page) {
       case 16: return run(cache_write_blocks_kernel<D, 16, 1>, 1);
       case 32: return run(cache_write_blocks_kernel<D, 32, 1>, 1);
-      case 64: return run(cache_write_blocks_kernel<D, 64, 4>, 4);
+      case 64: return run(cache_write_blocks_kernel<D, 64, W64>, W64);
       case 128: return run(cache_write_blocks_kernel<D, 128, 4>, 4);
       default: return run(cache_write_blocks_kernel<D, 256, 4>, 4);
     }

@@ -1,20 +1,30 @@
 // heart_cache_plan: pages, token ranges, slots and positions of a step's new tokens, from the requests' lengths.
 //
-// Four prefix sums over the requests say all: pages that go back, pages asked for, tokens of those whose pages are there, and
-// pages and tokens of those that are granted.  One workgroup computes them, a thread a request (sums saturate: lengths may be
+// Five prefix sums over the requests say all: pages that go back, pages asked for, tokens of those whose pages are there, and
+// pages and tokens of those that are granted.  One workgroup computes them, in three rounds (sums saturate: lengths may be
 // anything).  What they place -- pages back on the list, pages from it into the table, a slot and a position for each token -- is
 // independent, each item found by a search in the sums.
 //
-// Bound by latency: a chain of loads, three rounds of sums, loads from the list, stores.  A call of few tokens is one launch, one
-// of many three, as items are then dealt to the chip, and pages have to be back on the list before they are taken from it.
+// Bound by latency: chains of loads, each of which takes a microsecond where another XCD wrote what it reads, and launches.  So
+// sums that are searched lie in LDS, and there are as few launches as can be (struct PlanMode).
+#include <algorithm>
+
 #include "heart_internal.h"
 
 namespace heart {
 
-constexpr int kPlanThreads = 1024;   // of the workgroup that sums: requests at a time
-constexpr int kPlanGroups = 512;     // workgroups of 256 threads that place items
+// kAlone   few new tokens: one workgroup, one launch.
+// kShared  many of not too many requests: a first launch whose workgroups all compute the sums, and give pages back; what the
+//          sums come from stays as it is until the second, which places the rest.
+// kLarge   more requests than a workgroup holds: sums, pages back, the rest.
+enum PlanMode { kAlone, kShared, kLarge };
+constexpr int kPlanThreads = 1024;   // of a workgroup that sums
+constexpr int kPlanEach = 4;         // requests of a thread, where there are more than threads
+constexpr int kPlanHeld = kPlanThreads * kPlanEach;  // requests that a workgroup holds
+constexpr int kPlanSumGroups = 64;   // most workgroups that sum
+constexpr int kPlanGroups = 2048;    // most workgroups of 256 threads that place items
 constexpr int kPlanFew = 8192;       // new tokens, and
-constexpr int kPlanFewPages = 1 << 16;  // places in the table, that one workgroup places alone
+constexpr int kPlanFewPages = 1 << 18;  // places in the table, that one workgroup places alone
 
 struct PlanCall {
   int B, M, shift, n_pages, T;
@@ -82,54 +92,77 @@ __device__ __forceinline__ int last_before(int lo, int hi, uint32_t x, F &&first
   }
   return lo;
 }
+// The same for x0 + lane, of all B, by the whole wavefront: 64 places at a time for x0, then the 64 requests behind that one for
+// all lanes, and again 64 where that is not enough.  Few loads follow one another.
+template <typename F>
+__device__ __forceinline__ int last_before_wave(int B, uint32_t x0, int lane, F &&first) {
+  int lo = 0, n = B;
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lo + lane * step;
+    const bool before = lane * step < n && at < B && first(at) <= x0;
+    const int k = max(__popcll(__ballot(before)) - 1, 0);
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const uint32_t x = heart_op_umin(add_sat(x0, (uint32_t)lane), 0xfffffffeu);  // (never what stands for no request)
+  int b = lo;
+  for (int from = lo + 1;; from += 64) {
+    const uint32_t mine = from + lane < B ? first(from + lane) : 0xffffffffu;
+    int k = 0;
+#pragma unroll
+    for (int step = 32; step; step >>= 1)
+      if ((uint32_t)__shfl((int)mine, k + step - 1, 64) <= x) k += step;
+    if ((uint32_t)__shfl((int)mine, k, 64) <= x) ++k;
+    if (b == from - 1) b += k;  // (all that came before were passed)
+    if (!__any(b == from + 63)) return b;
+  }
+}
 
 __device__ __forceinline__ int pages_of(const PlanCall &c, int tokens) { return (int)(((unsigned)tokens + (1u << c.shift) - 1u) >> c.shift); }
 
-// Page i of those that go back: to the list, the first on top; its place in the table is empty, or will be taken.
-template <typename R>
-__device__ __forceinline__ void give_back(const PlanCall &c, const PlanTotals &all, uint32_t i, R &&req) {
-  const int b = last_before(0, c.B - 1, i, [&](int x) { return req(x).back; });
-  const PlanRequest r = req(b);
-  const int p = pages_of(c, r.kept) + (int)(i - r.back);
-  if (p >= r.own) return;  // (sums that saturate)
-  int *at = c.table + (long long)b * c.M + p;
-  const long long to = (long long)all.top - 1 - i;
-  if (to >= all.free) c.list[to] = *at;
-  const uint32_t next = b + 1 < c.B ? req(b + 1).taken : all.taken;
-  if ((uint32_t)(p - pages_of(c, r.kept)) >= next - r.taken) *at = -1;
+// A request as the items need it.
+struct PlanPlace {
+  int kept;
+  uint32_t first;  // of the items
+};
+
+// Page i of those that go back, of request b: to the list, the first on top.  (Its place in the table is empty, until it is taken.)
+__device__ __forceinline__ void give_back(const PlanCall &c, int n_free, int top, uint32_t i, int b, const PlanPlace &r) {
+  int *at = c.table + (long long)b * c.M + pages_of(c, r.kept) + (int)(i - r.first);
+  const long long to = (long long)top - 1 - i;
+  if (to >= n_free) c.list[to] = *at;
+  *at = -1;
 }
-// (i < all.taken <= all.top)
-__device__ __forceinline__ int page_taken(const PlanCall &c, const PlanTotals &all, uint32_t i) { return c.list[all.top - 1 - (int)i]; }
-template <typename R>
-__device__ __forceinline__ void take(const PlanCall &c, const PlanTotals &all, uint32_t i, R &&req) {
-  const int b = last_before(0, c.B - 1, i, [&](int x) { return req(x).taken; });
-  const PlanRequest r = req(b);
-  c.table[(long long)b * c.M + pages_of(c, r.kept) + (int)(i - r.taken)] = page_taken(c, all, i);
+// (i < the pages taken <= top)
+__device__ __forceinline__ int page_taken(const PlanCall &c, int top, uint32_t i) { return c.list[top - 1 - (int)i]; }
+// Page i of those that are taken, of request b.
+__device__ __forceinline__ void take(const PlanCall &c, int top, uint32_t i, int b, const PlanPlace &r) {
+  c.table[(long long)b * c.M + pages_of(c, r.kept) + (int)(i - r.first)] = page_taken(c, top, i);
 }
-// Token t, of one of the requests lo .. hi, or of none (t >= tokens).
-template <typename R, typename C>
-__device__ __forceinline__ void place(const PlanCall &c, const PlanTotals &all, int t, int tokens, int lo, int hi, R &&req, C &&cu) {
-  long long slot = -1;
-  int pos = -1;
-  if (t < tokens) {
-    const int b = last_before(lo, hi, (uint32_t)t, cu);
-    const PlanRequest r = req(b);
-    pos = r.kept + (t - (int)cu(b));
-    const int p = pos >> c.shift, had = pages_of(c, r.kept);
-    const int id = p < had ? c.table[(long long)b * c.M + p] : page_taken(c, all, r.taken + (uint32_t)(p - had));
-    if ((unsigned)id < (unsigned)c.n_pages) slot = ((long long)id << c.shift) + (pos & ((1 << c.shift) - 1));
-  }
+// Token t of request b, whose pages that are taken are those from `taken` on: its position and slot.
+__device__ __forceinline__ void find_token(const PlanCall &c, int top, int t, int b, const PlanPlace &r, uint32_t taken, int &pos, long long &slot) {
+  pos = r.kept + (t - (int)r.first);
+  const int p = pos >> c.shift, had = pages_of(c, r.kept);
+  const int id = p < had ? c.table[(long long)b * c.M + p] : page_taken(c, top, taken + (uint32_t)(p - had));
+  slot = (unsigned)id < (unsigned)c.n_pages ? ((long long)id << c.shift) + (pos & ((1 << c.shift) - 1)) : -1;
+}
+__device__ __forceinline__ void put_token(const PlanCall &c, int t, int pos, long long slot) {
   if (c.slots) c.slots[t] = slot;
   if (c.positions) c.positions[t] = pos;
 }
 
-// kAlone: of at most kPlanThreads requests, whose items the workgroup places itself.
-template <bool kAlone>
+// EACH: requests of a thread at a time.
+template <PlanMode kMode, int EACH>
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(const PlanCall c) {
+  static_assert(kMode != kAlone || EACH == 1, "a thread a request");
+  constexpr int CHUNK = kPlanThreads * EACH;
   __shared__ uint32_t wave_sum[2][2][kPlanThreads / 64];
-  __shared__ PlanRequest s_req[kAlone ? kPlanThreads : 1];
-  __shared__ int s_cu[kAlone ? kPlanThreads + 1 : 1];
+  __shared__ uint32_t s_back[kMode == kLarge ? 1 : CHUNK];  // pages that go back before a request's own, pages taken, tokens
+  __shared__ uint32_t s_taken[kMode == kAlone ? CHUNK : 1], s_first[kMode == kAlone ? CHUNK : 1];
+  __shared__ int s_kept[kMode == kLarge ? 1 : CHUNK];
   const int t = threadIdx.x;
+  const bool writes = kMode == kAlone || blockIdx.x == 0;  // (the others compute the same)
   const long long cap = (long long)c.M << c.shift;
   PlanSums sums{wave_sum, 0};
   const int n_free = min(max(*c.n_free, 0), c.n_pages);
@@ -139,9 +172,9 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(const PlanCall
     kept = c.keep ? min(max(c.keep[b], 0), kv) : kv;
     own = pages_of(c, kv);
   };
-  // (more requests than threads: all that goes back first)
+  // (more requests than the workgroup holds: all that goes back first)
   uint32_t back_all = 0;
-  if constexpr (!kAlone) {
+  if constexpr (kMode == kLarge) {
     uint32_t mine[2] = {0, 0}, unused[2], all[2];
     for (int b = t; b < c.B; b += kPlanThreads) {
       int kept, own;
@@ -151,85 +184,192 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(const PlanCall
     sums.scan(mine, unused, all);
     back_all = all[0];
   }
-  uint32_t back0 = 0, need0 = 0, asked0 = 0, taken0 = 0, tokens0 = 0;  // sums over the requests before this thousand
+  uint32_t back0 = 0, need0 = 0, asked0 = 0, taken0 = 0, tokens0 = 0;  // sums over the requests before this chunk
   int top = 0;
-  for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
-    const int b = b0 + t;
-    int kept = 0, own = 0, want = 0;
-    if (b < c.B) {
-      lengths(b, kept, own);
-      want = max(c.add[b], 0);
+  for (int b0 = 0; b0 < c.B; b0 += CHUNK) {
+    const int b = b0 + t * EACH;  // (the thread's first)
+    int kept[EACH], own[EACH], want[EACH];
+    uint32_t need[EACH], v[2] = {0, 0}, before[2], all[2];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      kept[e] = own[e] = want[e] = 0;
+      if (b + e < c.B) {
+        lengths(b + e, kept[e], own[e]);
+        want[e] = max(c.add[b + e], 0);
+      }
     }
-    const int had = pages_of(c, kept);
-    const bool fits = want > 0 && (long long)kept + want <= cap;
-    uint32_t v[2] = {(uint32_t)(own - had), fits ? (uint32_t)(pages_of(c, kept + want) - had) : 0u}, before[2], all[2];
-    const uint32_t need = v[1];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int had = pages_of(c, kept[e]);
+      if ((long long)kept[e] + want[e] > cap) want[e] = 0;  // (does not fit the table)
+      need[e] = (uint32_t)(pages_of(c, kept[e] + want[e]) - had);
+      v[0] = add_sat(v[0], (uint32_t)(own[e] - had));
+      v[1] = add_sat(v[1], need[e]);
+    }
     sums.scan(v, before, all);
-    const uint32_t back = add_sat(back0, before[0]);
-    const uint32_t asked = add_sat(add_sat(need0, before[1]), need);  // with its own
+    uint32_t back = add_sat(back0, before[0]), asked = add_sat(need0, before[1]);
     back0 = add_sat(back0, all[0]);
     need0 = add_sat(need0, all[1]);
-    if constexpr (kAlone) back_all = all[0];
+    if constexpr (kMode != kLarge) back_all = all[0];
     top = (int)min((unsigned long long)n_free + back_all, (unsigned long long)c.n_pages);
-    // pages are there
-    const bool paged = fits && (need == 0 || asked <= (uint32_t)top);
-    v[0] = paged ? (uint32_t)want : 0u;
-    v[1] = 0;
+    // pages are there, or none are needed
+    v[0] = v[1] = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      asked = add_sat(asked, need[e]);
+      if (need[e] > 0 && asked > (uint32_t)top) want[e] = 0;
+      v[0] = add_sat(v[0], (uint32_t)want[e]);
+    }
     sums.scan(v, before, all);
-    const bool given = paged && add_sat(add_sat(asked0, before[0]), (uint32_t)want) <= (uint32_t)c.T;
+    uint32_t tokens = add_sat(asked0, before[0]);
     asked0 = add_sat(asked0, all[0]);
-    v[0] = given ? need : 0u;
-    v[1] = given ? (uint32_t)want : 0u;
+    v[0] = v[1] = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      tokens = add_sat(tokens, (uint32_t)want[e]);
+      if (tokens > (uint32_t)c.T) want[e] = 0;
+      if (want[e] == 0) need[e] = 0;
+      v[0] += need[e];
+      v[1] += (uint32_t)want[e];
+    }
     sums.scan(v, before, all);
-    const uint32_t taken = taken0 + before[0], first = tokens0 + before[1];
+    uint32_t taken = taken0 + before[0], first = tokens0 + before[1];
     taken0 += all[0];
     tokens0 += all[1];
-    if (b < c.B) {
-      const PlanRequest r{kept, own, back, taken};
-      if constexpr (kAlone) {
-        s_req[b] = r;
-        s_cu[b] = (int)first;
-      } else {
-        c.req[b] = __builtin_bit_cast(int4, r);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      if (b + e >= c.B) break;
+      if constexpr (kMode != kLarge) {
+        s_back[b + e] = back;
+        s_kept[b + e] = kept[e];
       }
-      c.cu[b] = (int)first;
-      c.kv_len[b] = kept + (given ? want : 0);
+      if constexpr (kMode == kAlone) {
+        s_taken[b] = taken;
+        s_first[b] = first;
+        c.kv_len[b] = kept[e] + want[e];
+      } else if (writes) {
+        c.req[b + e] = __builtin_bit_cast(int4, PlanRequest{kept[e], own[e], back, taken});
+      }
+      if (writes) c.cu[b + e] = (int)first;
+      back = add_sat(back, (uint32_t)(own[e] - pages_of(c, kept[e])));
+      taken += need[e];
+      first += (uint32_t)want[e];
     }
   }
-  const PlanTotals all{n_free, top, back_all, taken0};
-  if (t == 0) {
+  if (writes && t == 0) {
     c.cu[c.B] = (int)tokens0;
-    *c.n_free = top - (int)taken0;
-    if constexpr (kAlone) s_cu[c.B] = (int)tokens0;
-    else c.req[c.B] = __builtin_bit_cast(int4, all);
+    if constexpr (kMode == kAlone) *c.n_free = top - (int)taken0;
+    else c.req[c.B] = __builtin_bit_cast(int4, PlanTotals{n_free, top, back_all, taken0});
   }
-  if constexpr (kAlone) {
+  if constexpr (kMode != kLarge) {
     __syncthreads();
-    auto req = [&](int b) -> const PlanRequest & { return s_req[b]; };
-    for (uint32_t i = t; i < all.back; i += kPlanThreads) give_back(c, all, i, req);
+    const unsigned long long step = (unsigned long long)gridDim.x * kPlanThreads;
+    for (unsigned long long i = blockIdx.x * (unsigned long long)kPlanThreads + t; i < back_all; i += step) {
+      const int b = last_before(0, c.B - 1, (uint32_t)i, [&](int x) { return s_back[x]; });
+      give_back(c, n_free, top, (uint32_t)i, b, PlanPlace{s_kept[b], s_back[b]});
+    }
+  }
+  if constexpr (kMode == kAlone) {
     __threadfence_block();
-    __syncthreads();  // the list is whole
-    for (uint32_t i = t; i < all.taken; i += kPlanThreads) take(c, all, i, req);
-    for (int i = t; i < c.T; i += kPlanThreads)
-      place(c, all, i, (int)tokens0, 0, c.B - 1, req, [&](int b) { return (uint32_t)s_cu[b]; });
+    __syncthreads();  // the list is whole, and places that are taken are empty
+    for (uint32_t i = t; i < taken0; i += kPlanThreads) {
+      const int b = last_before(0, c.B - 1, i, [&](int x) { return s_taken[x]; });
+      take(c, top, i, b, PlanPlace{s_kept[b], s_taken[b]});
+    }
+    for (int i = t; i < c.T; i += 2 * kPlanThreads) {
+      int pos[2] = {-1, -1};
+      long long slot[2] = {-1, -1};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int x = i + e * kPlanThreads;
+        if (x < (int)tokens0) {
+          const int b = last_before(0, c.B - 1, (uint32_t)x, [&](int y) { return s_first[y]; });
+          find_token(c, top, x, b, PlanPlace{s_kept[b], s_first[b]}, s_taken[b], pos[e], slot[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (i + e * kPlanThreads < c.T) put_token(c, i + e * kPlanThreads, pos[e], slot[e]);
+    }
   }
 }
+
+__device__ __forceinline__ PlanRequest plan_request(const PlanCall &c, int b) { return __builtin_bit_cast(PlanRequest, c.req[b]); }
 
 __global__ __launch_bounds__(256) void cache_plan_back_kernel(const PlanCall c) {
   const PlanTotals all = __builtin_bit_cast(PlanTotals, c.req[c.B]);
-  auto req = [&](int b) { return __builtin_bit_cast(PlanRequest, c.req[b]); };
+  const int lane = threadIdx.x & 63;
   const unsigned long long step = (unsigned long long)gridDim.x * 256;
-  for (unsigned long long i = blockIdx.x * 256u + threadIdx.x; i < all.back; i += step) give_back(c, all, (uint32_t)i, req);
+  for (unsigned long long i = blockIdx.x * 256u + (threadIdx.x & ~63u); i < all.back; i += step) {
+    const int b = last_before_wave(c.B, (uint32_t)i, lane, [&](int x) { return plan_request(c, x).back; });
+    const PlanRequest r = plan_request(c, b);
+    if (i + lane < all.back) give_back(c, all.free, all.top, (uint32_t)i + lane, b, PlanPlace{r.kept, r.back});
+  }
 }
 
-__global__ __launch_bounds__(256) void cache_plan_place_kernel(const PlanCall c) {
+// Pages taken and lengths (the first `takers` workgroups), and tokens.  kHeld: of at most kPlanHeld requests, whose sums are
+// searched in LDS.
+template <bool kHeld>
+__global__ __launch_bounds__(256) void cache_plan_place_kernel(const PlanCall c, int takers) {
+  __shared__ uint32_t s_first[kHeld ? kPlanHeld : 1];
   const PlanTotals all = __builtin_bit_cast(PlanTotals, c.req[c.B]);
-  auto req = [&](int b) { return __builtin_bit_cast(PlanRequest, c.req[b]); };
-  auto cu = [&](int b) { return (uint32_t)c.cu[b]; };
-  const uint32_t step = gridDim.x * 256, mine = blockIdx.x * 256 + threadIdx.x;
-  for (unsigned long long i = mine; i < all.taken; i += step) take(c, all, (uint32_t)i, req);
-  const int tokens = c.cu[c.B];
-  for (long long i = mine; i < c.T; i += step) place(c, all, (int)i, tokens, 0, c.B - 1, req, cu);
+  const int lane = threadIdx.x & 63;
+  const bool takes = (int)blockIdx.x < takers;
+  const uint32_t group = takes ? blockIdx.x : blockIdx.x - takers, step = (takes ? takers : gridDim.x - takers) * 256u;
+  const uint32_t mine = group * 256 + (threadIdx.x & ~63u);
+  auto sum = [&](int b) { return takes ? plan_request(c, b).taken : (uint32_t)c.cu[b]; };
+  if constexpr (kHeld) {
+#pragma unroll 4
+    for (int b = threadIdx.x; b < c.B; b += 256) s_first[b] = sum(b);
+    __syncthreads();
+  }
+  // the request of item i + lane (i below `n`)
+  auto request = [&](uint32_t i, uint32_t n, uint32_t &first) __attribute__((always_inline)) -> int {
+    if constexpr (kHeld) {
+      const int b = last_before(0, c.B - 1, heart_op_umin(i + lane, n - 1), [&](int x) { return s_first[x]; });
+      first = s_first[b];
+      return b;
+    } else {
+      const int b = last_before_wave(c.B, i, lane, sum);
+      first = sum(b);
+      return b;
+    }
+  };
+  if (takes) {
+    for (unsigned long long i = mine; i < all.taken; i += step) {
+      uint32_t first;
+      const int b = request((uint32_t)i, all.taken, first);
+      if (i + lane < all.taken) take(c, all.top, (uint32_t)i + lane, b, PlanPlace{plan_request(c, b).kept, first});
+    }
+    for (unsigned long long b = mine + lane; b < (unsigned)c.B; b += step)
+      c.kv_len[b] = plan_request(c, (int)b).kept + (c.cu[b + 1] - c.cu[b]);
+    if (mine + lane == 0) *c.n_free = all.top - (int)all.taken;
+    return;
+  }
+  // (two tokens of a thread at a time: what they load is on its way together)
+  const uint32_t tokens = (uint32_t)c.cu[c.B];
+  constexpr int N = 2;
+  for (unsigned long long i0 = mine; i0 < (unsigned)c.T; i0 += (unsigned long long)N * step) {
+    int pos[N];
+    long long slot[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t i = (uint32_t)i0 + e * step;  // (at most 2^30 and two steps)
+      pos[e] = -1;
+      slot[e] = -1;
+      if (i < tokens) {
+        uint32_t first;
+        const int b = request(i, tokens, first);
+        const PlanRequest r = plan_request(c, b);
+        if (i + lane < tokens) find_token(c, all.top, (int)i + lane, b, PlanPlace{r.kept, first}, r.taken, pos[e], slot[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t x = (uint32_t)i0 + e * step + lane;
+      if (x < (uint32_t)c.T) put_token(c, (int)x, pos[e], slot[e]);
+    }
+  }
 }
 
 static bool plan_alone(int B, int max_pages, int T) {
@@ -246,14 +386,25 @@ int launch_cache_plan(int B, int max_pages, int page, int n_pages, int T, const 
   const PlanCall c{B, max_pages, __builtin_ctz((unsigned)page), n_pages, T, keep, add, kv_len, page_table, free_pages, n_free, cu_q,
                    positions, slots, (int4 *)workspace};
   if (plan_alone(B, max_pages, T)) {
-    hipLaunchKernelGGL(cache_plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, st, c);
+    hipLaunchKernelGGL((cache_plan_kernel<kAlone, 1>), dim3(1), dim3(kPlanThreads), 0, st, c);
     return check_launch("cache_plan_kernel");
   }
-  hipLaunchKernelGGL(cache_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, st, c);
+  // (what the items are at most, as far as it is known here)
+  auto groups = [](long long items, int each, int most) { return dim3((unsigned)std::min((items + each - 1) / each, (long long)most)); };
+  const long long back = std::min((long long)n_pages, (long long)B * max_pages);
+  const dim3 take = groups(std::max((long long)B, std::min(back, (long long)T / page + B)), 256, kPlanSumGroups);
+  const dim3 place(take.x + groups((T + 1ll) / 2, 256, kPlanGroups).x);
+  if (B <= kPlanHeld) {
+    hipLaunchKernelGGL((cache_plan_kernel<kShared, kPlanEach>), groups(back, kPlanThreads, kPlanSumGroups), dim3(kPlanThreads), 0, st, c);
+    if (int rc = check_launch("cache_plan_kernel")) return rc;
+    hipLaunchKernelGGL(cache_plan_place_kernel<true>, place, dim3(256), 0, st, c, (int)take.x);
+    return check_launch("cache_plan_place_kernel");
+  }
+  hipLaunchKernelGGL((cache_plan_kernel<kLarge, kPlanEach>), dim3(1), dim3(kPlanThreads), 0, st, c);
   if (int rc = check_launch("cache_plan_kernel")) return rc;
-  hipLaunchKernelGGL(cache_plan_back_kernel, dim3(kPlanGroups), dim3(256), 0, st, c);
+  hipLaunchKernelGGL(cache_plan_back_kernel, groups(back, 256, kPlanGroups), dim3(256), 0, st, c);
   if (int rc = check_launch("cache_plan_back_kernel")) return rc;
-  hipLaunchKernelGGL(cache_plan_place_kernel, dim3(kPlanGroups), dim3(256), 0, st, c);
+  hipLaunchKernelGGL(cache_plan_place_kernel<false>, place, dim3(256), 0, st, c, (int)take.x);
   return check_launch("cache_plan_place_kernel");
 }
 
