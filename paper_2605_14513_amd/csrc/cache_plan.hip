@@ -23,8 +23,9 @@ constexpr int kPlanEach = 4;         // requests of a thread, where there are mo
 constexpr int kPlanHeld = kPlanThreads * kPlanEach;  // requests that a workgroup holds
 constexpr int kPlanSumGroups = 64;   // most workgroups that sum
 constexpr int kPlanGroups = 2048;    // most workgroups of 256 threads that place items
-constexpr int kPlanFew = 8192;       // new tokens, and
-constexpr int kPlanFewPages = 1 << 18;  // places in the table, that one workgroup places alone
+// New tokens that one workgroup places alone.  us alone, shared: 8 requests of 800 tokens 5.4, 9.1, of 8000 8.8, 9.0; 256 of 4096
+// 8.4, 10.6, of 8192 12.4, 11.0; 1000 of 4000 9.6, 12.2, of 8000 14.1, 12.6.  And places in the table, all of which may go back.
+constexpr int kPlanFew = 6000, kPlanFewPages = 1 << 18;
 
 struct PlanCall {
   int B, M, shift, n_pages, T;

@@ -48,8 +48,8 @@ def check(add, kv, keep, table, free, n_free, page, T, what="", workspace="auto"
 
 
 @pytest.mark.parametrize("B,M,page,T", [
-    (1, 1, 16, 1), (1, 1, 16, 0), (1, 500, 64, 4680), (2, 9, 16, 40), (64, 20, 16, 300), (65, 20, 32, 4000), (1023, 6, 16, 3000), (1024, 5, 32, 8192),
-    (1024, 6, 16, 8193), (1025, 6, 16, 3000), (3000, 4, 16, 9000), (17, 200, 256, 30000), (300, 300, 16, 5000), (5, 3, 128, 2)])
+    (1, 1, 16, 1), (1, 1, 16, 0), (1, 500, 64, 4680), (2, 9, 16, 40), (64, 20, 16, 300), (65, 20, 32, 4000), (1023, 6, 16, 3000), (1024, 5, 32, 6000),
+    (1024, 6, 16, 6001), (1025, 6, 16, 3000), (3000, 4, 16, 9000), (4096, 3, 16, 9000), (4097, 3, 16, 9000), (9000, 2, 16, 20000), (2, 140000, 16, 50), (17, 200, 256, 30000), (300, 300, 16, 5000), (5, 3, 128, 2)])
 def test_random_requests(B, M, page, T):
     for seed in range(4):
         r = random.Random(1000 * B + 10 * M + seed)
