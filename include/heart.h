@@ -381,12 +381,16 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * Precision as heart_block_sparse_attn: bf16 products, fp32 sums, logits scaled and exponentiated in fp32, weights rounded
  * to bf16 for the second contraction (the row sum adds them unrounded), or, where a sequence has 16 rows (new tokens times G)
  * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values they stand for (as part
- * of the weights, v's exponents, where these are two bf16: below an exponent of 32 they lose bits).  Rows from kv_len on may
- * hold anything, pages of nobody too; a NaN or an infinity among the first kv_len tokens may also reach queries that do not see
- * it.  (Weights are up to 2^8 before the division by their sum: 2^8 sum |v| over a query's keys has to stay below 2^128, and
- * v's exponents below 247.)  out must not overlap q.  T Hq is at most 2^30.
+ * of the weights, v's exponents, where these are two bf16: below an exponent of 32 they lose bits).  Of int8 the codes are
+ * multiplied and the scales applied in fp32 where a sequence has 16 rows or less (64, where there is little to be read) and weights
+ * are two bf16; else products are of f16: queries by their row's power of two (elements below 2^-32 of the largest lose bits), k's
+ * codes, v's values by a power of two of the tile (those under scales below 2^-26 of its largest lose bits), weights rounded to
+ * f16 (below 2^-21 of the largest they lose bits).  Rows from kv_len on may
+ * hold anything, pages of nobody too; a NaN or an infinity among the first kv_len tokens (int8: a scale that is one) may also
+ * reach queries that do not see it.  (Weights are up to 2^8, of int8 2^15, before the division by their sum: that times sum |v|
+ * over a query's keys has to stay below 2^128, and v's exponents below 247.)  out must not overlap q.  T Hq is at most 2^30.
  * workspace: DEVICE, 16-byte aligned, of at least heart_cache_attn_workspace_bytes(cache, T, Hq) bytes (which looks at
- * B, H, D alone), or NULL.  With it the keys of few queries (of at most 256 sequences) are divided over the chip, into parts
+ * type, B, H, D alone), or NULL.  With it the keys of few queries (of at most 256 sequences) are divided over the chip, into parts
  * that depend on all lengths of the call; results are those without it up to rounding, and the same for the same call.
  * Contents irrelevant on entry and undefined on return; two calls that run concurrently must not share one.
  */

@@ -501,7 +501,8 @@ def heart_cache_attn_workspace_bytes(q, k_cache, page_table) -> int:
     """Bytes of workspace for heart_cache_attn of q [T,Hq,D] (0 where it has no use for one)."""
     if q.dim() != 3 or k_cache.dim() != 4 or page_table.dim() != 2:
         raise ValueError("q must be [T,Hq,D], k_cache [n_pages,H,page,D] and page_table [B,max_pages]")
-    c = HeartCache(H=k_cache.shape[1], D=k_cache.shape[3], B=page_table.shape[0])
+    c = HeartCache(H=k_cache.shape[1], D=k_cache.shape[3], B=page_table.shape[0],
+                   type=HEART_CACHE_INT8 if k_cache.dtype == torch.int8 else HEART_CACHE_BF16)
     return int(load_library().heart_cache_attn_workspace_bytes(ctypes.byref(c), int(q.shape[0]), int(q.shape[1])))
 
 

@@ -886,11 +886,14 @@ static Division divide(int B, long long n_items) {
   return {kTail, 1, (int)n_items - r, best, (long long)r * best};
 }
 
-size_t cache_attn_workspace_bytes(int B, int H, int D, int T, int Hq) {
-  if (cache_attn_few(B, H, T, Hq)) return cache_attn_few_workspace_bytes(B, H, D, T, Hq);
+size_t cache_attn_workspace_bytes(int type, int B, int H, int D, int T, int Hq) {
+  const size_t few = cache_attn_few_workspace_bytes(B, H, D, T, Hq);
+  if (cache_attn_few(B, H, T, Hq)) return few;
   const Division d = divide(B, most_items(kTile, B, H, T, Hq));
   const size_t part = D == 128 ? kPartFloats<128> : kPartFloats<64>;
-  return d.mode == kWhole ? 0 : kPlaces * sizeof(int4) + (size_t)d.slots() * 4 * part * sizeof(float);
+  const size_t many = d.mode == kWhole ? 0 : kPlaces * sizeof(int4) + (size_t)d.slots() * 4 * part * sizeof(float);
+  // (which kernel it is goes by the page tables' room too, which is not known here)
+  return type == HEART_CACHE_INT8 && (long long)T * (Hq / H) <= (long long)kIntRows * B && few > many ? few : many;
 }
 
 template <int D, CacheKind kKind>
@@ -933,7 +936,8 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   a.qt = qs[0], a.qh = qs[1], a.ot = os[0], a.oh = os[1];
   a.H = c.H, a.G = Hq / c.H, a.causal = causal, a.window = window;
   a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.D)) * 1.4426950408889634f;
-  if (cache_attn_few(c.B, c.H, T, Hq)) return launch_cache_attn_few(c, T, Hq, a, workspace, st);
+  if (c.type == HEART_CACHE_INT8 ? cache_attn_int8_few(c, T, Hq) : cache_attn_few(c.B, c.H, T, Hq))
+    return launch_cache_attn_few(c, T, Hq, a, workspace, st);
   const long long items = most_items(kTile, c.B, c.H, T, Hq);
   if (items > kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   Division d = divide(c.B, items);

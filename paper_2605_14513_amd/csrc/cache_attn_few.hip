@@ -737,6 +737,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
 // 4000 48.9 / 51.8, in e4m3 31.4 / 39.4, 64 of 1000 44.8 / 43.3, in e4m3 27.2 / 31.6; 24 rows (two tiles): 18 to 35 % slower
 // than that where one sequence is divided, 5 % faster to 9 % slower in batches.
 bool cache_attn_few(int B, int H, int T, int Hq) { return (long long)T * (Hq / H) <= (long long)kFewTile * B; }
+// The same where tiles have little to read, of int8 (keys: what the page tables have room for): tiles at most, all in one round of
+// places, their keys together, and of one.  us of this kernel and of the other, D = 128: 24 rows, 8 heads of 1000 keys 12.6 / 18.8, of
+// 4000 17.1 / 20.4, 16 sequences 23.1 / 28.9 and 53.8 / 46.3; 64 rows, 8 heads of 300 keys 12.4 / 15.9, of 4000 20.7 / 20.8, 16 sequences
+// 18.0 / 25.3 and 91.9 / 54.8; 64 sequences, 24 rows, 300 keys 25.6 / 21.1; 64 rows, two heads of 16000 keys 35.5 / 28.4.
+constexpr long long kIntTiles = 640, kIntKeys = 5 << 16, kIntLongest = 4096;
+bool cache_attn_int8_few(const heart_cache &c, int T, int Hq) {
+  if (cache_attn_few(c.B, c.H, T, Hq)) return true;
+  const long long tiles = most_items(kFewTile, c.B, c.H, T, Hq), room = (long long)c.max_pages * c.page;
+  return (long long)T * (Hq / c.H) <= (long long)kIntRows * c.B && tiles <= kIntTiles && room <= kIntLongest && tiles * room <= kIntKeys;
+}
 static bool few_divides(int B, long long items) { return B <= kSplitSeqs && items <= kFewItems; }
 
 size_t cache_attn_few_workspace_bytes(int B, int H, int D, int T, int Hq) {

@@ -416,7 +416,7 @@ int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, con
 
 size_t heart_cache_attn_workspace_bytes(const heart_cache *c, int T, int Hq) {
   if (!c || c->B <= 0 || c->H <= 0 || (c->D != 64 && c->D != 128) || T <= 0 || Hq <= 0 || Hq % c->H != 0) return 0;
-  return cache_attn_workspace_bytes(c->B, c->H, c->D, T, Hq);
+  return cache_attn_workspace_bytes(c->type, c->B, c->H, c->D, T, Hq);
 }
 
 size_t heart_cache_plan_workspace_bytes(int B, int max_pages, int T) {

@@ -315,7 +315,7 @@ int launch_cache_read(const heart_cache &c, int N, void *k, const long long ks[3
 int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const long long qs[2], const int *cu_q, int causal,
                       int window, float scale, void *out, const long long os[2], float *lse, void *workspace,
                       hipStream_t st);
-size_t cache_attn_workspace_bytes(int B, int H, int D, int T, int Hq);
+size_t cache_attn_workspace_bytes(int type, int B, int H, int D, int T, int Hq);
 int launch_cache_plan(int B, int max_pages, int page, int n_pages, int T, const int *keep, const int *add, int *kv_len,
                       int *page_table, int *free_pages, int *n_free, int *cu_q, long long *slots, int *positions, void *workspace,
                       hipStream_t st);

@@ -45,9 +45,24 @@ def test_a_write_has_less_than_2_to_the_32_threads(lib):  # noqa: F811
     assert calls(lib, c, T=1 << 29)["write"]() == EUNSUPPORTED and b"too many rows" in lib.heart_last_error()
 
 
-def test_workspace_of_attention_does_not_go_by_the_type(lib):  # noqa: F811
-    size = lambda **kw: lib.heart_cache_attn_workspace_bytes(ctypes.byref(cache(**kw)), 3, 4)  # noqa: E731
-    assert size(type=INT8, k_exp=F, v_exp=F) == size() > 0
+def test_workspace_of_attention(lib):  # noqa: F811
+    """Where either kernel may be meant, of int8 caches, the size is enough for both; else it is that of other types."""
+    size = lambda T, Hq, **kw: lib.heart_cache_attn_workspace_bytes(ctypes.byref(cache(**kw)), T, Hq)  # noqa: E731
+    int8 = dict(type=INT8, k_exp=F, v_exp=F)
+    assert size(3, 4, **int8) == size(3, 4) > 0 and size(3 * 33, 4, **int8) == size(3 * 33, 4) > 0
+    for T, Hq, B in ((3 * 9, 4, 3), (3 * 32, 4, 3), (64 * 16, 2, 64)):
+        few = size(B, 2, B=B)
+        assert size(T, Hq, B=B, **int8) == max(few, size(T, Hq, B=B)) >= few > 0
+    assert size(300 * 20, 2, B=300, **int8) == size(300 * 20, 2, B=300)  # (more sequences than are divided)
+
+
+def test_binding_asks_for_the_workspace_of_the_type(lib):  # noqa: F811
+    import paper_2605_14513_amd as heart
+
+    q, table = bf(16 * 3, 16, 64), torch.zeros((3, 4), dtype=torch.int32)
+    size = lambda t: heart.heart_cache_attn_workspace_bytes(q, torch.zeros((9, 8, 16, 64), dtype=t), table)  # noqa: E731
+    want = lambda t: lib.heart_cache_attn_workspace_bytes(ctypes.byref(cache(B=3, H=8, D=64, type=t, k_exp=F, v_exp=F)), 48, 16)  # noqa: E731
+    assert size(torch.int8) == want(INT8) and size(torch.bfloat16) == want(0)
 
 
 def test_binding_refuses_what_does_not_belong_together(lib):  # noqa: F811
