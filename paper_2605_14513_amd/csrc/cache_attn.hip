@@ -362,14 +362,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     if constexpr (kInts)
       raw_unit[is_v] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(units[is_v]), i & 63));
   };
-  // (int8) V in f16 is in units of a power of two, 2^5 of which are above the largest scale of the part
+  // (int8) V in f16 is in units of a power of two, 2^5 of which are above the largest scale of the part: known where the page ids
+  // of its first stages are, of long parts after a look at the others
   float v_unit = 1.f, to_v_unit = 1.f;
-  if constexpr (kInts) {
-    uint32_t top = 0;
-    if (n_stage > 0) {
+  auto find_v_unit = [&]() __attribute__((always_inline)) {
+    const uint32_t mine = __float_as_uint(units[1]);
+    uint32_t top = mine < 0x7f800000u ? mine : 0u;
+    if (n_stage > 63) {
       const float *scales = reinterpret_cast<const float *>(c.v.exp);
 #pragma unroll 4
-      for (int p = (key0 >> c.s.page_shift) + t; p <= (end_key - 1) >> c.s.page_shift; p += 256) {
+      for (int p = ((key0 + 63 * kStage) >> c.s.page_shift) + t; p <= (end_key - 1) >> c.s.page_shift; p += 256) {
         const int id = cache_page(c.s, wk.b, p << c.s.page_shift);
         const uint32_t u = __float_as_uint(scales[(long long)max(id, 0) * c.H + wk.h]);
         top = heart_op_umax(top, id >= 0 && u < 0x7f800000u ? u : 0u);
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     const uint32_t up = heart_op_umin(258u - (top >> 23), 253u);  // 2^(4 - exponent of the largest)
     to_v_unit = __uint_as_float(up << 23);
     v_unit = __uint_as_float((254u - up) << 23);
-  }
+  };
   auto store_codes = [&](int is_v, int ii, int p, int buf) __attribute__((always_inline)) {
     const int r = wave * 16 + ii * RPC + crow, f = swizzle(is_v, r);
     unsigned char *dst = smem + (2 * is_v + buf) * TILE_B + r * ROWB;
@@ -647,6 +649,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
       load_codes(0, 0);
       load_codes(1, 0);
     }
+    if constexpr (kInts) find_v_unit();
     bring_all(0, 0);
     bring_all(1, 1);
     publish();
