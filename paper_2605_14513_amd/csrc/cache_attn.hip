@@ -164,8 +164,10 @@ __device__ __forceinline__ f16x2_t codes_up(uint32_t turned) {
   return __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, turned, kUpper ? 0x04030402u : 0x04010400u));
 }
 
-template <int D, CacheKind kKind, CacheMode kMode>
-__global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
+template <int D, CacheKind kKind, CacheMode kMode, int WAVES = kTile / 32>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCall c) {
+  constexpr int TILE = 32 * WAVES, THREADS = 64 * WAVES, ROWS = kStage / WAVES;  // rows of a tile, rows that a wavefront brings of a stage
+  static_assert(WAVES == 4 || (kKind == kInt8 && kMode == kWhole), "wide tiles: of int8, not divided");
   constexpr bool kCodes = kKind != kBf16, kInts = kKind == kInt8;
   constexpr int DT = D / 32;             // 32-wide d tiles of the output
   constexpr int KS = D / 16;             // k-steps of the first product
@@ -174,10 +176,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   constexpr int RPB = 16 / CPR;          // rows per 256 bytes (one pass over the 64 banks)
   constexpr int TILE_B = kStage * ROWB;  // bytes of a stage of K or V
   constexpr int RPI = 64 / CPR;          // rows that an LDS-direct load covers
-  constexpr int IPW = 16 / RPI;          // such loads per wavefront and stage
+  constexpr int IPW = ROWS / RPI;          // such loads per wavefront and stage
   constexpr int LPC = D / 16;            // (codes) lanes that hold a row, 16 codes each
   constexpr int RPC = 64 / LPC;          // rows of one load
-  constexpr int CPW = 16 / RPC;          // loads per wavefront and stage
+  constexpr int CPW = ROWS / RPC;          // loads per wavefront and stage
   constexpr int SO = D + 8;              // LDS row stride of the output staging (elements)
   // weights are at most 2^(kTop + 8), and the largest of a row is 2^kTop at least
   constexpr float kTop = kInts ? 7.f : 0.f, kRescaleSlack = kTop + 8.f;
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   // LDS: [K stage 0][K stage 1][V stage 0][V stage 1], reused for the output at the end
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ __align__(16) float s_unit[kInts ? 2 : 1][4];  // (int8) scales of a K stage's rows, 16 each
-  __shared__ uint32_t s_top[4];                             // (int8) V's largest scale
+  __shared__ uint32_t s_top[WAVES];                             // (int8) V's largest scale
   const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
 
   const int t = threadIdx.x;
@@ -218,20 +220,20 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
       }
     }
     item_at(c, i, c.n_items, tile, wk.h);
-    wk.b = seq_of_tile<kTile>(c, tile, lane);
-    wk.m = tile - tile_start<kTile>(c, wk.b);
+    wk.b = seq_of_tile<TILE>(c, tile, lane);
+    wk.m = tile - tile_start<TILE>(c, wk.b);
   }
   wk.b = __builtin_amdgcn_readfirstlane(wk.b);
   wk.m = __builtin_amdgcn_readfirstlane(wk.m);
   const Seq s = seq_of(c, wk.b);
-  const int tiles = tiles_of<kTile>(c, s);
+  const int tiles = tiles_of<TILE>(c, s);
   if (wk.m < 0 || wk.m >= tiles) return;
-  if constexpr (kInParts) rec = (tile_start<kTile>(c, wk.b) + wk.m) * c.H + wk.h;
+  if constexpr (kInParts) rec = (tile_start<TILE>(c, wk.b) + wk.m) * c.H + wk.h;
   else wk.m = tiles - 1 - wk.m;  // (later tiles see more keys: first)
-  const int rows = s.n * c.G, r0 = wk.m * kTile;
+  const int rows = s.n * c.G, r0 = wk.m * TILE;
   int lo, hi, first_key, end_key, ignore;
   seen_by(c, s, s.pos0 + r0 / c.G, first_key, ignore);
-  seen_by(c, s, s.pos0 + min(r0 + kTile - 1, rows - 1) / c.G, ignore, end_key);
+  seen_by(c, s, s.pos0 + min(r0 + TILE - 1, rows - 1) / c.G, ignore, end_key);
   const int tile_end = __builtin_amdgcn_readfirstlane(end_key);  // keys from here on no row of the tile sees: zeros
   int stage0 = first_key / kStage, n_stage = max((end_key + kStage - 1) / kStage - stage0, 0);
   int parts = 1;
@@ -290,7 +292,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   auto load_ids = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
     for (int is_v = 0; is_v < 2; ++is_v) {
-      const int key = key0 + (base + lane) * kStage - 32 * is_v + 16 * wave;
+      const int key = key0 + (base + lane) * kStage - 32 * is_v + ROWS * wave;
       ids[is_v] = -1;
       if (base + lane <= n_stage && key >= 0 && key < tile_end) ids[is_v] = cache_page(c.s, wk.b, key);
       if constexpr (kInts) {
@@ -303,12 +305,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
   // rows that are there of the wavefront's 16 of a stage, the address of the first one's element 0 and exponent
   auto rows_at = [&](int is_v, int i, uint64_t &addr, uint64_t &exp_addr) __attribute__((always_inline)) -> int {
     const CacheTensor &x = is_v ? c.v : c.k;
-    const int key = key0 + i * kStage - 32 * is_v + 16 * wave;
+    const int key = key0 + i * kStage - 32 * is_v + ROWS * wave;
     const int id = __builtin_amdgcn_readlane(ids[is_v], i & 63);
     const int off = key & in_page;
     addr = (uint64_t)(x.p + max(id, 0) * x.page + wk.h * x.head + off * (long long)x.row);
     if constexpr (kKind == kE4m3) exp_addr = (uint64_t)(x.exp + ((((long long)max(id, 0) * c.H + wk.h) << c.s.page_shift) + off));
-    return id < 0 ? 0 : min(tile_end - key, 16);
+    return id < 0 ? 0 : min(tile_end - key, ROWS);
   };
   // LDS-direct loads (bf16): one instruction moves 16 bytes per lane to 1 KB of consecutive LDS; lane l lands at chunk
   // position l % CPR of row l / CPR and therefore fetches chunk (l % CPR) ^ f(row).
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
 #pragma unroll
       for (int ii = 0; ii < IPW; ++ii) {
         const int r = ii * RPI + lane / CPR;
-        dma_off[is_v][ii] = (uint32_t)r * (is_v ? c.v.row : c.k.row) + (uint32_t)(((lane % CPR) ^ swizzle(is_v, wave * 16 + r)) * 16);
+        dma_off[is_v][ii] = (uint32_t)r * (is_v ? c.v.row : c.k.row) + (uint32_t)(((lane % CPR) ^ swizzle(is_v, wave * ROWS + r)) * 16);
       }
   }
   u32x4_t dma_rs[2];
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     if (n_stage > 63) {
       const float *scales = reinterpret_cast<const float *>(c.v.exp);
 #pragma unroll 4
-      for (int p = ((key0 + 63 * kStage) >> c.s.page_shift) + t; p <= (end_key - 1) >> c.s.page_shift; p += 256) {
+      for (int p = ((key0 + 63 * kStage) >> c.s.page_shift) + t; p <= (end_key - 1) >> c.s.page_shift; p += THREADS) {
         const int id = cache_page(c.s, wk.b, p << c.s.page_shift);
         const uint32_t u = __float_as_uint(scales[(long long)max(id, 0) * c.H + wk.h]);
         top = heart_op_umax(top, id >= 0 && u < 0x7f800000u ? u : 0u);
@@ -380,13 +382,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     top = wave_max_u32(top);
     if (lane == 0) s_top[wave] = top;
     __syncthreads();
-    top = heart_op_umax(heart_op_umax(s_top[0], s_top[1]), heart_op_umax(s_top[2], s_top[3]));
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = heart_op_umax(top, s_top[w]);
     const uint32_t up = heart_op_umin(258u - (top >> 23), 253u);  // 2^(4 - exponent of the largest)
     to_v_unit = __uint_as_float(up << 23);
     v_unit = __uint_as_float((254u - up) << 23);
   };
   auto store_codes = [&](int is_v, int ii, int p, int buf) __attribute__((always_inline)) {
-    const int r = wave * 16 + ii * RPC + crow, f = swizzle(is_v, r);
+    const int r = wave * ROWS + ii * RPC + crow, f = swizzle(is_v, r);
     unsigned char *dst = smem + (2 * is_v + buf) * TILE_B + r * ROWB;
     const u32x4_t x = raw[is_v][ii];
     if constexpr (kInts) {
@@ -402,7 +405,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
         y[2 * w + 1] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(b, u2, less2) : b + less1);
       }
       *reinterpret_cast<u32x4_t *>(dst + (((2 * cchunk + p) ^ f) * 16)) = y;
-      if (!is_v && ii == 0 && p == 0) s_unit[buf][wave] = raw_unit[0];
+      // (where two wavefronts have 16 rows, the first's are there if any are)
+      if (!is_v && ii == 0 && p == 0 && wave * ROWS % 16 == 0) s_unit[buf][wave * ROWS / 16] = raw_unit[0];
       return;
     }
     const float unit = unit_of(raw_exp[is_v][ii]);
@@ -734,7 +738,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
     const Row at = row_of(c, s, wk.h, row);
     c.lse[(long long)at.head * c.s.T + at.token] = l_tot == 0.f ? ninf : (m_ref + log2f(l_tot)) * 0.6931471805599453f;
   }
-  uint16_t *sO = reinterpret_cast<uint16_t *>(smem);  // [kTile][SO]
+  uint16_t *sO = reinterpret_cast<uint16_t *>(smem);  // [TILE][SO]
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -745,7 +749,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const AttnCall c) {
       *reinterpret_cast<u32x2_t *>(sO + (wave * 32 + l32) * SO + dt * 32 + 8 * g + 4 * hf) = pk;
     }
   __syncthreads();
-  constexpr int OCH = kTile * CPR / 256, STEP_R = 256 / CPR;
+  constexpr int OCH = TILE * CPR / THREADS, STEP_R = THREADS / CPR;
 #pragma unroll
   for (int it = 0; it < OCH; ++it) {
     const int r = t / CPR + it * STEP_R;
@@ -889,6 +893,18 @@ static Division divide(int B, long long n_items) {
   return {kTail, 1, (int)n_items - r, best, (long long)r * best};
 }
 
+// int8, D = 128: tiles of 256 rows, eight wavefronts, that share what it takes to turn codes into f16 (VALU instructions of a wavefront
+// and stage 274 -> 230).  They are not divided, so: where long sequences have four tiles each, on average, and the last round of
+// the chip's 256 places is full but for a seventh.  us of tiles of 128 and of 256, 4680 queries of 32760 keys: 40 heads (760 tiles)
+// 3366 / 2994, 24 (456) 2152 / 1895, 12 (228) 1076 / 974, but 16 (304) 1303 / 1819; six ragged prompts of up to 2048 tokens, 40 on 8
+// heads, 12000 keys 755 / 739; 4680 keys, 40 heads, 313 / 316; 64 of up to 256 tokens, 8 heads 135 / 149.
+constexpr int kWideTile = 256, kWidePlaces = 256;
+static bool wide_tiles(const heart_cache &c, int T, int Hq) {
+  if (c.type != HEART_CACHE_INT8 || c.D != 128 || (long long)c.max_pages * c.page <= kBrief) return false;
+  const long long tiles = most_items(kWideTile, c.B, c.H, T, Hq), round = (tiles + kWidePlaces - 1) / kWidePlaces * kWidePlaces;
+  return (long long)T * (Hq / c.H) >= 4ll * kWideTile * c.B && 7 * tiles >= 6 * round;
+}
+
 size_t cache_attn_workspace_bytes(int type, int B, int H, int D, int T, int Hq) {
   const size_t few = cache_attn_few_workspace_bytes(B, H, D, T, Hq);
   if (cache_attn_few(B, H, T, Hq)) return few;
@@ -900,18 +916,22 @@ size_t cache_attn_workspace_bytes(int type, int B, int H, int D, int T, int Hq) 
 }
 
 template <int D, CacheKind kKind>
-static int launch_t(const AttnCall &c, const Division &d, hipStream_t st) {
+static int launch_t(const AttnCall &c, const Division &d, bool wide, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
-  constexpr int lds = 4 * kStage * D * 2, staging = kTile * (D + 8) * 2, bytes = lds > staging ? lds : staging;
-  auto run = [&](auto mode, long long grid) -> int {
-    auto kern = cache_attn_kernel<D, kKind, decltype(mode)::value>;
+  auto run_waves = [&](auto mode, long long grid, auto waves) -> int {
+    constexpr int W = decltype(waves)::value;
+    constexpr int lds = 4 * kStage * D * 2, staging = 32 * W * (D + 8) * 2, bytes = lds > staging ? lds : staging;
+    auto kern = cache_attn_kernel<D, kKind, decltype(mode)::value, W>;
     static DeviceFlags attr_set;  // per instantiation: the attribute is per function and device
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
       return fail(HEART_EHIP, "hipFuncSetAttribute(max dynamic LDS %d): %s", bytes, hipGetErrorString(e));
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, st, c);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), bytes, st, c);
     return check_launch("cache_attn_kernel");
   };
+  auto run = [&](auto mode, long long grid) -> int { return run_waves(mode, grid, std::integral_constant<int, kTile / 32>{}); };
+  if constexpr (kKind == kInt8 && D == 128)
+    if (wide) return run_waves(std::integral_constant<CacheMode, kWhole>{}, c.n_items, std::integral_constant<int, kWideTile / 32>{});
   if (d.mode == kWhole) return run(std::integral_constant<CacheMode, kWhole>{}, c.n_items);
   if (d.mode == kParts) {
     const int rc = c.s.B <= 64 ? run(std::integral_constant<CacheMode, kParts>{}, d.slots())
@@ -953,7 +973,8 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
     d.rounds = 1;
   }
   if (!workspace) d = {kWhole, 1, 0, 1, 0};
-  a.n_items = (int)items;
+  const bool wide = wide_tiles(c, T, Hq);
+  a.n_items = (int)(wide ? most_items(kWideTile, c.B, c.H, T, Hq) : items);
   a.rounds = d.rounds;
   a.whole = d.whole;
   a.tail = d.tail;
@@ -961,8 +982,8 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
   a.part = workspace ? (float *)(a.items + kPlaces) : nullptr;
   auto of_kind = [&](auto dim) -> int {
     constexpr int D = decltype(dim)::value;
-    if (c.type == HEART_CACHE_INT8) return launch_t<D, kInt8>(a, d, st);
-    return c.type == HEART_CACHE_E4M3 ? launch_t<D, kE4m3>(a, d, st) : launch_t<D, kBf16>(a, d, st);
+    if (c.type == HEART_CACHE_INT8) return launch_t<D, kInt8>(a, d, wide, st);
+    return c.type == HEART_CACHE_E4M3 ? launch_t<D, kE4m3>(a, d, false, st) : launch_t<D, kBf16>(a, d, false, st);
   };
   return c.D == 128 ? of_kind(std::integral_constant<int, 128>{}) : of_kind(std::integral_constant<int, 64>{});
 }

@@ -208,6 +208,55 @@ def test_either_kernel_around_its_limits(D):
             check(c, new_q(B * n, H * G, D), [n] * B, cu=B % 2 == 0, workspace=ws)
 
 
+# (44 heads of five tiles of 256 rows: one round that is nearly full, where the page table has room for more than 5120 tokens)
+@pytest.mark.parametrize("B,n,kvs,G,page,causal,window", [
+    (1, 1024, [1100], 1, 16, 1, 0), (1, 1037, [1037], 1, 64, 1, 0), (1, 1024, [1029], 1, 16, 0, 0), (1, 1024, [1203], 1, 32, 300, 0),
+    (1, 1024, [2047], 1, 16, 1, 77), (1, 257, [1016], 4, 128, 100, 130), (1, 1024, [4093], 1, 16, 1, 0), (2, 1100, [1111, 1100], 1, 16, 1, 0)])
+def test_wide_tiles(B, n, kvs, G, page, causal, window):
+    """Tiles of 256 rows give the same bits as those of 128 (the same cache under a page table with less room); lengths that end inside
+    the sixteen rows of two wavefronts among them."""
+    H, D = 44 if B == 1 else 24, 128
+    c = Blocks(kvs, H, D, page, seed=n, room=5200, spread=9)
+    q = new_q(B * n, H * G, D)
+    out, lse = torch.zeros((2, B * n, H * G, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, H * G, B * n), device="cuda")
+    short = c.page_table[:, :-(-max(kvs) // page)].contiguous()
+    for i, table in enumerate((c.page_table, short)):
+        print(f"cache_attn int8 wide B={B} n={n} kvs={kvs} G={G} page={page} causal={causal} window={window} room {table.shape[1] * page}", flush=True)
+        heart.heart_cache_attn(q.cuda(), c.stored["k"], c.stored["v"], table, c.kv_len, causal=causal, window=window, out=out[i], lse=lse[i],
+                               workspace=None, **c.scale_args())
+        torch.cuda.synchronize()
+    assert torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])
+    some = [0, H * G - 1]  # (the definition of two heads)
+    one = Blocks(kvs, H, D, page, seed=n, room=5200, spread=9, device="cpu")
+    for h in some:
+        for w in ("k", "v"):
+            one.codes[w], one.scales[w] = c.codes[w][:, h // G:h // G + 1], c.scales[w][:, h // G:h // G + 1]
+        one.H = 1
+        want, want_lse, tol, ltol = tolerance(one, q[:, h:h + 1], [n] * B, causal, window)
+        assert_near(out[0][:, h:h + 1], want, tol, "out")
+        assert_near(lse[0][h:h + 1], want_lse, ltol, "lse")
+
+
+def test_wide_tiles_of_anything():
+    """Ragged ranges, pages that are none, a scale that is NaN and lengths that are none, of tiles of 256 rows."""
+    H, D, kvs, qs = 16, 128, [1300, 1100, 0], [1290, 1100, 700]
+    c = Blocks(kvs, H, D, 16, seed=1, room=5200)
+    c.table_cpu[0, 3], c.table_cpu[1, 60], c.table_cpu[0, 81] = -1, c.n_pages, 2**31 - 1
+    c.page_table.copy_(c.table_cpu)
+    c.scale["k"][c.table_cpu[1, 2], 5] = math.nan
+    q = new_q(sum(qs) + 9, H, D)
+    got = []
+    for table in (c.page_table, c.page_table[:, :100].contiguous()):
+        out, lse = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, q.shape[0]), 5.0, device="cuda")
+        heart.heart_cache_attn(q.cuda(), c.stored["k"], c.stored["v"], table, c.kv_len, cu_q=ends(qs), out=out, lse=lse, workspace=None, **c.scale_args())
+        torch.cuda.synchronize()
+        got.append((out, lse))
+    assert torch.equal(got[0][0].view(torch.int16), got[1][0].view(torch.int16)) and torch.equal(got[0][1].view(torch.int32), got[1][1].view(torch.int32))
+    out, lse = got[0]
+    assert out[1290 + 40:2390, 5].isnan().all() and not out[:1290].isnan().any() and not out[:, :5].isnan().any()
+    assert (out[2390:3090] == 0).all() and (lse[:, 2390:3090] == -math.inf).all() and (out[3090:] == 5.0).all()
+
+
 def test_many_parts_and_tails():
     """Sizes at which the keys of tiles are divided in each way: few tiles, two rounds of parts, a divided last round."""
     for B, n, kv, H, G in ((1, 300, 9000, 2, 1), (3, 130, 5000, 4, 4), (70, 33, 300, 2, 4), (1, 1200, 6000, 60, 1), (1, 16, 20000, 1, 1)):
