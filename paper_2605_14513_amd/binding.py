@@ -449,7 +449,7 @@ def _units(k_cache, k_exp, v_exp, k_scale, v_scale):
     """The exponents of a cache, or the scales of an int8 one."""
     if k_scale is None and v_scale is None:
         return k_exp, v_exp
-    if k_cache.dtype != torch.int8:
+    if getattr(k_cache, "dtype", torch.int8) != torch.int8:
         raise ValueError("k_scale, v_scale: only an int8 cache has scales")
     if k_exp is not None or v_exp is not None:
         raise ValueError("k_exp, v_exp: an int8 cache has scales, no exponents")
@@ -509,7 +509,7 @@ def heart_cache_attn_workspace_bytes(q, k_cache, page_table) -> int:
 def heart_cache_attn(q, k_cache, v_cache, page_table, kv_len, cu_q=None, k_exp=None, v_exp=None, causal: int = 1,
                      window: int = 0, scale: float = 0.0, out=None, lse=None, workspace="auto", k_scale=None, v_scale=None):
     """Attention of the new tokens' queries (bf16 [T,Hq,D]) over the cache, which holds their keys and values already (the
-    cache's arguments: heart_cache_write); returns bf16 out like q (rows behind cu_q[B] are left as they are in a given out,
+    cache's arguments, k_scale and v_scale of an int8 one among them: heart_cache_write); returns bf16 out like q (rows behind cu_q[B] are left as they are in a given out,
     and hold anything in a new one).
 
     causal: 0 a query sees the whole sequence, n > 0 the blocks of n positions up to its own; window: only the last so

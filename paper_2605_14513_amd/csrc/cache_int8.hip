@@ -63,20 +63,17 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
 }
 
 // WAVES wavefronts for a job, a workgroup of 256 threads for 4 / WAVES jobs.
-#ifndef W64
-#define W64 4
-#endif
 template <int D, int PAGE, int WAVES>
-__global__ __launch_bounds__(256) void cache_write_blocks_kernel(BlockSide k, BlockSide v, CacheSeqs s, int H, long long n_jobs) {
+__global__ __launch_bounds__(256) void cache_write_blocks_kernel(BlockSide k, BlockSide v, CacheSeqs s, int H, int n_jobs) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, ROWS = PAGE / WAVES, NI = ROWS / RPI;  // lanes of a row, rows of a load and a wavefront
   static_assert(NI >= 1 && NI * RPI * WAVES == PAGE, "a page is a whole number of loads");
   __shared__ uint32_t s_top[4];
   const int lane = threadIdx.x & 63, sub = lane / LPR, col = lane % LPR;
   const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long at = (long long)blockIdx.x * (4 / WAVES) + wave / WAVES;
+  const int at = (int)blockIdx.x * (4 / WAVES) + wave / WAVES;
   if (at >= n_jobs) return;  // (all of a job's wavefronts)
   // heads fastest: a token's rows are read together
-  const int h = (int)(at % H), is_v = (int)(at / H & 1), job = (int)(at / H / 2);
+  const int rest = (int)((unsigned)at / (unsigned)H), h = at - rest * H, is_v = rest & 1, job = rest >> 1;
   const BlockSide &c = is_v ? v : k;
   const int b = seq_of_job(s, job, lane);
   const int first = s.cu ? s.cu[b] : b * s.per, n = (s.cu ? s.cu[b + 1] : first + s.per) - first;
@@ -161,7 +158,7 @@ int launch_cache_write_blocks(const heart_cache &c, int T, const void *k, const 
   const CacheSeqs seqs = cache_seqs(c, T, cu_q);
   auto run = [&](auto kern, int waves) -> int {
     const long long groups = (jobs * waves + 3) / 4;
-    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), 0, st, sk, sv, seqs, c.H, jobs);
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), 0, st, sk, sv, seqs, c.H, (int)jobs);
     return check_launch("cache_write_blocks_kernel");
   };
   auto of_page = [&](auto d) -> int {
@@ -169,7 +166,7 @@ int launch_cache_write_blocks(const heart_cache &c, int T, const void *k, const 
     switch (c.page) {
       case 16: return run(cache_write_blocks_kernel<D, 16, 1>, 1);
       case 32: return run(cache_write_blocks_kernel<D, 32, 1>, 1);
-      case 64: return run(cache_write_blocks_kernel<D, 64, W64>, W64);
+      case 64: return run(cache_write_blocks_kernel<D, 64, 4>, 4);
       case 128: return run(cache_write_blocks_kernel<D, 128, 4>, 4);
       default: return run(cache_write_blocks_kernel<D, 256, 4>, 4);
     }
