@@ -13,11 +13,14 @@
 // fragment read; V as it is, its powers of two go into the weights, which are multiplied by them before they are
 // rounded (a power of two rounds nothing).
 //
-// Dividing the keys: struct Shares.  The workgroup that finds all parts of a tile there adds them up.
+// int8: codes are bf16 as they are, scales (one for 16 rows, which lie in a page) are factors of the logits and of the weights.
 //
-// 64 ragged sequences of up to 8192 tokens, 8 key heads of 128, e4m3 (385 MB) 74 us, 5.2 TB/s; one of 120001 tokens, bf16 (492 MB)
-// 84 us, 5.8 TB/s; 64 of 16384, bf16 (4.3 GB) 6.8 TB/s, of 32768 in e4m3 6.6 (a plain read 7.1).  One of
-// 1000 tokens, two heads: 9.9 us, bound by latency.
+// Dividing the keys: struct Shares.  The workgroup that finds all parts of a tile there adds them up.  Little is not divided
+// (int8, kFewAll).
+//
+// 64 ragged sequences of up to 8192 tokens, 8 key heads of 128, e4m3 (385 MB) and int8 74 us, 5.2 TB/s; one of 120001 tokens, bf16
+// (492 MB) 84 us, 5.8 TB/s, int8 (246 MB) 53, 4.6; 64 of 16384, bf16 (4.3 GB) 6.8 TB/s, of 32768 in e4m3 6.6 (a plain read 7.1).  One of
+// 1000 tokens, two heads: 9.9 us, int8 8.9, bound by latency.
 #include <type_traits>
 
 #include "cache_attn_device.h"
@@ -25,6 +28,8 @@
 namespace heart {
 
 constexpr int kFewTile = 16;     // rows of a workgroup
+constexpr int kFewWaves = 4;     // its wavefronts, and
+constexpr int kFewAll = 16;      // those of a workgroup that has all keys of a tile at once, a slice a wavefront
 constexpr int kFewStage = 128;   // keys that shares are measured in
 constexpr int kFewMin = 2;       // shortest share, in stages
 constexpr int kFewCut = 1;       // fewest stages of a part: a cut closer to an end of its tile goes there
@@ -113,7 +118,7 @@ struct Shares {
   }
 };
 
-template <int D, CacheKind kKind>
+template <int D, CacheKind kKind, int WAVES>
 struct FewShape {
   static constexpr bool kCodes = kKind != kBf16;
   static constexpr int ROWB = kCodes ? D : 2 * D;        // bytes of a row
@@ -121,7 +126,7 @@ struct FewShape {
   static constexpr int NT = SK / 16;                     // key tiles of 16
   static constexpr int TENSOR_B = SK * ROWB;             // bytes of a slice of K or V
   static constexpr int SLICE_B = 2 * TENSOR_B + (kCodes ? 256 : 0);
-  static constexpr int WAVE_B = 2 * SLICE_B;             // double-buffered
+  static constexpr int WAVE_B = (WAVES > kFewWaves ? 1 : 2) * SLICE_B;  // double-buffered, but where there is one slice
   static constexpr int NI = 16 * ROWB / 1024;            // LDS-direct loads of 16 rows
 };
 
@@ -134,9 +139,11 @@ __device__ __forceinline__ u32x2_t ints_to_bf16(uint32_t w) {
 }
 
 // SEQS: sequences a lane where the keys are divided, 0 = they are not
-template <int D, CacheKind kKind, int SEQS>
-__global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c) {
-  using F = FewShape<D, kKind>;
+template <int D, CacheKind kKind, int SEQS, int WAVES = kFewWaves>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4 > 2 ? WAVES / 4 : 2) void cache_attn_few_kernel(const AttnCall c) {
+  using F = FewShape<D, kKind, WAVES>;
+  constexpr bool kAll = WAVES > kFewWaves;  // (all keys at once)
+  static_assert(!kAll || SEQS == 0, "not divided");
   constexpr bool kCodes = F::kCodes, kInts = kKind == kInt8;
   constexpr bool kSplit = SEQS > 0;
   constexpr int TILE = kFewTile, ROWB = F::ROWB, SK = F::SK, NT = F::NT, NI = F::NI;
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   constexpr int PER = 2 * NLOAD + (kCodes ? 1 : 0);    // all of a slice
   constexpr float ninf = -__builtin_inff(), kSlack = 8.f;
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ float s_ref[4][TILE], s_sum[4][TILE];
+  __shared__ float s_ref[WAVES][TILE], s_sum[WAVES][TILE];
   __shared__ bool s_all;
   const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
@@ -289,7 +296,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   }
   const int key0 = __builtin_amdgcn_readfirstlane(stage0 * kFewStage + wave * SK);  // of this wavefront's slice 0
   end_key = __builtin_amdgcn_readfirstlane(end_key);
-  const int n_slice = __builtin_amdgcn_readfirstlane(max((end_key - key0 + 4 * SK - 1) / (4 * SK), 0));
+  const int n_slice = __builtin_amdgcn_readfirstlane(max((end_key - key0 + WAVES * SK - 1) / (WAVES * SK), 0));
 
   int lo, hi;  // keys that this lane's row sees of the part
   seen_by(c, s, s.pos0 + at0.token(min(l16, n_rows - 1)), lo, hi);
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   auto load_ids = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const long long key = key0 + (long long)(base + lane) * (4 * SK) + 16 * n;
+      const long long key = key0 + (long long)(base + lane) * (WAVES * SK) + 16 * n;
       ids[n] = key < end_key ? cache_page(c.s, b, (int)key) : -1;
     }
   };
@@ -315,13 +322,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   const uint32_t wave_lds = smem_lds + (uint32_t)(wave * F::WAVE_B);
   unsigned char *const wave_mem = smem + wave * F::WAVE_B;
   // (half stages times 128 keys: bytes of K and V)
-  const bool once = !kSplit || (long long)sh.total * (128 * ROWB) > kFewOnce;
+  const bool once = !kAll && (!kSplit || (long long)sh.total * (128 * ROWB) > kFewOnce);
   // K (V) of slice i to buffer i & 1
   auto bring = [&](int is_v, int i) __attribute__((always_inline)) {
     const CacheTensor &x = is_v ? c.v : c.k;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int key = key0 + i * (4 * SK) + 16 * n, off = key & in_page;
+      const int key = key0 + i * (WAVES * SK) + 16 * n, off = key & in_page;
       const int id = i < n_slice ? __builtin_amdgcn_readlane(ids[n], i & 63) : -1;
       const uint64_t addr = (uint64_t)(x.p + max(id, 0) * x.page + head * x.head + off * (long long)x.row);
       const int there = id < 0 ? 0 : min(tile_end - key, 16);
@@ -360,7 +367,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
         id = n == m ? id_m : id;
       }
       id = max(id, 0);
-      const int key = key0 + i * (4 * SK) + 16 * n;
+      const int key = key0 + i * (WAVES * SK) + 16 * n;
       const uint8_t *base = dw >= (kInts ? NT : 4 * NT) ? c.v.exp : c.k.exp;
       const uint8_t *addr = kInts ? base + ((long long)id * c.H + head) * 4
                                   : base + ((((long long)id * c.H + head) << c.s.page_shift) + (key & in_page) + 4 * (dw & 3));
@@ -394,13 +401,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
     bring(0, 0);
     bring_exps(0, 0);
     bring(1, 0);
-    bring(0, 1);
-    bring_exps(1, 1);
-    bring(1, 1);
-    for (int i = 0; i < n_slice; ++i) {
+    if constexpr (!kAll) {
+      bring(0, 1);
+      bring_exps(1, 1);
+      bring(1, 1);
+    }
+    for (int i = 0; i < (kAll ? 1 : n_slice); ++i) {
       const unsigned char *sk = wave_mem + (i & 1) * F::SLICE_B, *sv = sk + F::TENSOR_B, *se = sk + 2 * F::TENSOR_B;
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NLOAD + PER) : "memory");  // K and exponents of slice i are there
-      const int key = key0 + i * (4 * SK);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NLOAD + (kAll ? 0 : PER)) : "memory");  // K and exponents of slice i are there
+      const int key = key0 + i * (WAVES * SK);
       // ---- S^T ------------------------------------------------------------------------------
       Frag8 kf[NT][KS];
       float vu[NT][4];  // (codes) powers of two of V's rows 16 n + 4 g + 0..3, or their scale
@@ -443,9 +452,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the fragments are in registers: their buffer is free)
-      if (((i + 2) & 63) == 0) load_ids(i + 2);
-      bring(0, i + 2);
-      bring_exps(i + 2, 2);
+      if constexpr (!kAll) {
+        if (((i + 2) & 63) == 0) load_ids(i + 2);
+        bring(0, i + 2);
+        bring_exps(i + 2, 2);
+      }
       f32x4_t x[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -511,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
         }
       }
       // ---- O^T ------------------------------------------------------------------------------------
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER + NLOAD + (kCodes ? 1 : 0)) : "memory");  // V of slice i is there
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAll ? 0 : PER + NLOAD + (kCodes ? 1 : 0)) : "memory");  // V of slice i is there
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
@@ -545,7 +556,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      bring(1, i + 2);
+      if constexpr (!kAll) bring(1, i + 2);
 #pragma unroll
       for (int n = 0; n < NT; ++n) named[0][n] = named[1][n], named[1][n] = named[2][n];
     }
@@ -585,16 +596,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(const AttnCall c
   auto part_rsrc = [&](int slot) __attribute__((always_inline)) -> __amdgpu_buffer_rsrc_t {
     return __builtin_amdgcn_make_buffer_rsrc(c.part + (size_t)slot * kFewPart<D>, 0, (int)(kFewPart<D> * sizeof(float)), 0x00020000);
   };
-  for (int i = t; i < n_rows * CH; i += 256) {
+  for (int i = t; i < n_rows * CH; i += 64 * WAVES) {
     const int r = i / CH, ch = i % CH;
     float ref = ninf;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) ref = fmaxf(ref, s_ref[w][r]);
+    for (int w = 0; w < WAVES; ++w) ref = fmaxf(ref, s_ref[w][r]);
     const float fin = ref == ninf ? 0.f : ref;
     float l = 0.f;
     f32x4_t y0 = {0.f, 0.f, 0.f, 0.f}, y1 = y0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_ref[w][r] - fin);
       const float *src = so + (size_t)w * (F::WAVE_B / 4) + r * D;
       l = fmaf(s_sum[w][r], f, l);
@@ -747,6 +758,11 @@ bool cache_attn_int8_few(const heart_cache &c, int T, int Hq) {
   const long long tiles = most_items(kFewTile, c.B, c.H, T, Hq), room = (long long)c.max_pages * c.page;
   return (long long)T * (Hq / c.H) <= (long long)kIntRows * c.B && tiles <= kIntTiles && room <= kIntLongest && tiles * room <= kIntKeys;
 }
+// int8: a workgroup of sixteen wavefronts has a tile, whose keys (by the room of the page tables) are a slice of 4 KB for each at most:
+// nothing is divided, so no parts have to meet, and no loop.  One a CU.  us, divided (or four wavefronts) and so: one token of 1000 keys, two
+// heads of 64 11.3 / 8.9, 16 sequences of 64 keys, 8 heads 8.7 / 6.8, of 1000 14.5 / 10.5; 8 rows, 8 heads of 128, 480 keys 11.9 / 8.1; 32
+// sequences of 200 keys, 8 heads (384 items) 8.7 / 11.1.
+constexpr long long kFewAllItems = 256;
 static bool few_divides(int B, long long items) { return B <= kSplitSeqs && items <= kFewItems; }
 
 size_t cache_attn_few_workspace_bytes(int B, int H, int D, int T, int Hq) {
@@ -755,19 +771,22 @@ size_t cache_attn_few_workspace_bytes(int B, int H, int D, int T, int Hq) {
 }
 
 template <int D, CacheKind kKind>
-static int launch_few_t(const AttnCall &c, bool split, long long grid, hipStream_t st) {
+static int launch_few_t(const AttnCall &c, bool split, bool all, long long grid, hipStream_t st) {
   const int dev = current_device();
   if (dev < 0) return fail(HEART_EHIP, "heart_cache_attn: cannot identify the current device");
-  constexpr int bytes = 4 * FewShape<D, kKind>::WAVE_B;
-  static_assert(bytes >= (256 / (D / 8)) * (D + 2) * 4, "sums of the parts fit the LDS");
-  auto run = [&](auto seqs) -> int {
-    auto kern = cache_attn_few_kernel<D, kKind, decltype(seqs)::value>;
+  auto run_waves = [&](auto seqs, auto waves) -> int {
+    constexpr int W = decltype(waves)::value, bytes = W * FewShape<D, kKind, W>::WAVE_B;
+    static_assert(bytes >= (256 / (D / 8)) * (D + 2) * 4, "sums of the parts fit the LDS");
+    auto kern = cache_attn_few_kernel<D, kKind, decltype(seqs)::value, W>;
     static DeviceFlags attr_set;  // per instantiation: the attribute is per function and device
     if (hipError_t e = set_max_lds_once(attr_set, dev, reinterpret_cast<const void *>(kern), bytes))
       return fail(HEART_EHIP, "hipFuncSetAttribute(max dynamic LDS %d): %s", bytes, hipGetErrorString(e));
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, st, c);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), bytes, st, c);
     return check_launch("cache_attn_few_kernel");
   };
+  if constexpr (kKind == kInt8)
+    if (all) return run_waves(std::integral_constant<int, 0>{}, std::integral_constant<int, kFewAll>{});
+  auto run = [&](auto seqs) -> int { return run_waves(seqs, std::integral_constant<int, kFewWaves>{}); };
   if (!split) return run(std::integral_constant<int, 0>{});
   return c.s.B <= 64 ? run(std::integral_constant<int, 1>{}) : run(std::integral_constant<int, kSplitSeqs / 64>{});
 }
@@ -777,8 +796,9 @@ int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, voi
   if (items > kMostGroups) return fail(HEART_EUNSUPPORTED, "heart_cache_attn: grid too large");
   const long long stages = ((long long)a.s.cap + kFewStage - 1) / kFewStage;
   const bool split = workspace && few_divides(hc.B, items) && stages <= (1ll << 27) / items;  // (sums of lengths fit 32 bits)
+  const bool all = hc.type == HEART_CACHE_INT8 && a.s.cap <= kFewAll * (4096 / hc.D) && items <= kFewAllItems;
   long long grid = items;
-  if (split) {
+  if (split && !all) {
     const long long most = items * ((stages + kFewMin - 1) / kFewMin);  // parts at most
     grid = most < kFewPlaces ? most : kFewPlaces;
     a.flags = (unsigned long long *)workspace;
@@ -787,8 +807,8 @@ int launch_cache_attn_few(const heart_cache &hc, int T, int Hq, AttnCall &a, voi
   }
   auto of_kind = [&](auto d) -> int {
     constexpr int D = decltype(d)::value;
-    if (hc.type == HEART_CACHE_INT8) return launch_few_t<D, kInt8>(a, split, grid, st);
-    return hc.type == HEART_CACHE_E4M3 ? launch_few_t<D, kE4m3>(a, split, grid, st) : launch_few_t<D, kBf16>(a, split, grid, st);
+    if (hc.type == HEART_CACHE_INT8) return launch_few_t<D, kInt8>(a, split, all, grid, st);
+    return hc.type == HEART_CACHE_E4M3 ? launch_few_t<D, kE4m3>(a, split, false, grid, st) : launch_few_t<D, kBf16>(a, split, false, grid, st);
   };
   return hc.D == 128 ? of_kind(std::integral_constant<int, 128>{}) : of_kind(std::integral_constant<int, 64>{});
 }

@@ -16,7 +16,7 @@ def new_q(T, Hq, D, seed=1):
 
 
 def check(c, q, qs, causal=1, window=0, scale=0.0, workspace="auto", cu=True, weight=2.0**-11, what=""):
-    print(f"cache_attn int8 qs={qs} kvs={c.lens} Hq={q.shape[1]} H={c.H} D={c.D} page={c.page} causal={causal} window={window} "
+    print(f"cache_attn int8 B={len(qs)} qs={qs[:6]} kvs={c.lens[:6]} Hq={q.shape[1]} H={c.H} D={c.D} page={c.page} causal={causal} window={window} "
           f"workspace={workspace} {what}", flush=True)
     T, Hq, D = q.shape
     if T * (Hq // c.H) <= 16 * len(qs):  # (few rows: weights of two bf16, scales in fp32)
@@ -151,6 +151,26 @@ def test_what_is_not_finite(n, workspace):
         ok[n + 1, 3] = False
         assert_near(out[ok], want[ok], tol[ok], "out")
         assert_near(lse.t()[ok], want_lse.t()[ok], ltol.t()[ok], "lse")
+
+
+@pytest.mark.parametrize("D,room", [(64, 1024), (128, 512), (64, 1040), (128, 528)])
+def test_short_sequences(D, room):
+    """All keys of a tile at once, where the page tables have room for no more, and one page more: empty and full sequences, windows,
+    pages that are none, a scale that is NaN, many sequences."""
+    for B, H, G, n in ((4, 3, 1, 1), (4, 3, 5, 3), (5, 1, 16, 1), (200, 1, 1, 1), (3, 2, 8, 7)):
+        kvs = [room, 0, 1, room - 17, 33][:B] + [1 + 37 * b % room for b in range(5, B)]
+        kvs = [max(0, k - 16) if room % 64 else k for k in kvs]
+        c = Blocks(kvs, H, D, 16, seed=B, room=room)
+        for causal, window in ((1, 0), (1, 45), (0, 0), (100, 0)):
+            check(c, new_q(B * n, H * G, D), [n] * B, causal, window, cu=B % 2 == 0)
+        c.table_cpu[0, 5], c.table_cpu[min(3, B - 1), 0] = -1, c.n_pages
+        c.page_table.copy_(c.table_cpu)
+        check(c, new_q(B * n, H * G, D), [n] * B, workspace=None)
+        for w in ("k", "v"):
+            bad = Blocks(kvs, H, D, 16, seed=B, room=room)
+            bad.scale[w][bad.table_cpu[0, 7], 0] = math.nan
+            out = heart.heart_cache_attn(new_q(B * n, H * G, D).cuda(), *bad.args(), **bad.scale_args()).cpu()
+            assert out[:n, :G].isnan().all() and not out[n:].isnan().any() and not out[:, G:].isnan().any()
 
 
 @pytest.mark.parametrize("scale", [2.0, 1e-3])
