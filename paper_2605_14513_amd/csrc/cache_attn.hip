@@ -346,7 +346,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
   // codes: a stage in registers, written to LDS as 16-bit values
   u32x4_t raw[2][CPW];
   uint32_t raw_exp[2][CPW];
-  float raw_unit[2];  // (int8) of the wavefront's 16 rows
+  float raw_unit[2];      // (int8) of the wavefront's rows
+  f16x2_t v_mul, v_less;  // (int8) V's scale in units of v_unit, and what its codes are too large by, of the stage that is stored
   const int crow = lane / LPC, cchunk = lane % LPC;
   auto load_codes = [&](int is_v, int i) __attribute__((always_inline)) {
     const uint32_t stride = is_v ? c.v.row : c.k.row;
@@ -394,15 +395,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
     const u32x4_t x = raw[is_v][ii];
     if constexpr (kInts) {
       // K as the codes are (its scales go into the logits), V times its scale
-      const _Float16 u = (_Float16)(raw_unit[1] * to_v_unit), less = (_Float16)-1152.f * u;
-      const f16x2_t u2 = {u, u}, less2 = {less, less}, less1 = {(_Float16)-1152.f, (_Float16)-1152.f};
+      if (is_v && ii == 0 && p == 0) {
+        const _Float16 u = (_Float16)(raw_unit[1] * to_v_unit), less = (_Float16)-1152.f * u;
+        v_mul = f16x2_t{u, u};
+        v_less = f16x2_t{less, less};
+      }
+      const f16x2_t k_less = {(_Float16)-1152.f, (_Float16)-1152.f};
       u32x4_t y;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         const uint32_t turned = x[2 * p + w] ^ 0x80808080u;
         const f16x2_t a = codes_up<false>(turned), b = codes_up<true>(turned);
-        y[2 * w] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(a, u2, less2) : a + less1);
-        y[2 * w + 1] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(b, u2, less2) : b + less1);
+        y[2 * w] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(a, v_mul, v_less) : a + k_less);
+        y[2 * w + 1] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(b, v_mul, v_less) : b + k_less);
       }
       *reinterpret_cast<u32x4_t *>(dst + (((2 * cchunk + p) ^ f) * 16)) = y;
       // (where two wavefronts have 16 rows, the first's are there if any are)
@@ -540,7 +545,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
   constexpr int UB = 16 / KS;  // micro-ops of a B slot
   constexpr int UC = 8 / DT;   // micro-ops of a C slot m < DT
   // (int8) what turns accumulators of the slice of position g into logits relative to the reference: factors of its two
-  // groups of 16 keys (no smaller than a normal number, so that -inf stays -inf), and the reference
+  // groups of 16 keys, and the reference.  (Factors are no smaller than a normal number, so that -inf stays -inf; compared as
+  // whole numbers, so that a NaN stays one.)
   float factor[2], less = 0.f;
   auto load_factors = [&](int g) __attribute__((always_inline)) {
     if constexpr (kInts) {
@@ -548,8 +554,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
       const f32x2_t u = *reinterpret_cast<const f32x2_t *>(&s_unit[(n >> 1) & 1][(n & 1) * 2]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float x = u[i] * row_unit;
-        factor[i] = x < 1.17549435e-38f ? 1.17549435e-38f : x;
+        factor[i] = __int_as_float(max(__float_as_int(u[i] * row_unit), 0x00800000));
       }
     }
   };
