@@ -167,7 +167,7 @@ __device__ __forceinline__ f16x2_t codes_up(uint32_t turned) {
 template <int D, CacheKind kKind, CacheMode kMode, int WAVES = kTile / 32>
 __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCall c) {
   constexpr int TILE = 32 * WAVES, THREADS = 64 * WAVES, ROWS = kStage / WAVES;  // rows of a tile, rows that a wavefront brings of a stage
-  static_assert(WAVES == 4 || (kKind == kInt8 && kMode == kWhole), "wide tiles: of int8, not divided");
+  static_assert(WAVES == 4 || (kKind == kInt8 && (kMode == kWhole || kMode == kTail)), "wide tiles: of int8, those of a last round divided");
   constexpr bool kCodes = kKind != kBf16, kInts = kKind == kInt8;
   constexpr int DT = D / 32;             // 32-wide d tiles of the output
   constexpr int KS = D / 16;             // k-steps of the first product
@@ -724,7 +724,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
   if (kSplit && parts > 1) {
     // ---- part of a tile: unnormalised output and its softmax state, as the lanes hold them ----
     if (!active) return;
-    float *dst = c.part + ((size_t)wk.slot * 4 + wave) * kPartFloats<D>;
+    float *dst = c.part + ((size_t)wk.slot * WAVES + wave) * kPartFloats<D>;
     dst[64 * 16 * DT + lane] = m_ref;
     dst[64 * 16 * DT + 64 + lane] = l_run;
     f32x4_t *o4 = reinterpret_cast<f32x4_t *>(dst);
@@ -772,26 +772,26 @@ constexpr int kMergeGroups = 4, kMergeParts = 4;  // groups, parts of a group in
 // Bound by latency (the parts come from the L2s and the memory-side cache): the parts are dealt to four groups of
 // wavefronts, four parts at a time each, and the groups' sums meet in LDS (8 queries of 32000 keys, 3 key heads in 125
 // parts each, D = 64: the call takes 28 us, 53 with one group).
-template <int D, CacheMode kMode>
+template <int D, CacheMode kMode, int WAVES = kTile / 32>
 __global__ __launch_bounds__(D * 2 * kMergeGroups) void cache_attn_merge_kernel(const AttnCall c) {
   constexpr float ninf = -__builtin_inff();
-  constexpr int DT = D / 32, NP = kMergeParts;
+  constexpr int DT = D / 32, NP = kMergeParts, TILE = 32 * WAVES;
   __shared__ float meet[kMergeGroups - 1][DT][18][64];
   const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const int dt = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) % DT);
   const int group = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) / DT);
-  const int wave = (int)(blockIdx.x % 4), item = (int)(blockIdx.x / 4);
+  const int wave = (int)(blockIdx.x % WAVES), item = (int)(blockIdx.x / WAVES);
   int tile, h;
   if constexpr (kMode == kTail) item_at(c, c.whole + item, c.n_items, tile, h);
   else tile = item / c.H, h = item % c.H;
-  const int b = seq_of_tile<kTile>(c, tile, lane);
-  int m = __builtin_amdgcn_readfirstlane(tile - tile_start<kTile>(c, b));
+  const int b = seq_of_tile<TILE>(c, tile, lane);
+  int m = __builtin_amdgcn_readfirstlane(tile - tile_start<TILE>(c, b));
   const Seq s = seq_of(c, b);
-  const int tiles = tiles_of<kTile>(c, s);
+  const int tiles = tiles_of<TILE>(c, s);
   if (m < 0 || m >= tiles) return;
   if constexpr (kMode == kTail) m = tiles - 1 - m;
-  const int rows = s.n * c.G, row = m * kTile + wave * 32 + l32;
-  if (m * kTile + wave * 32 >= rows) return;
+  const int rows = s.n * c.G, row = m * TILE + wave * 32 + l32;
+  if (m * TILE + wave * 32 >= rows) return;
   const int4 it = c.items[item];
   if (it.y <= 1) return;
   float ref = ninf, l = 0.f;
@@ -803,7 +803,7 @@ __global__ __launch_bounds__(D * 2 * kMergeGroups) void cache_attn_merge_kernel(
     f32x4_t x[NP][4];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const float *src = c.part + ((size_t)(it.x + min(s0 + kMergeGroups * i, it.y - 1) * it.z) * 4 + wave) * kPartFloats<D>;
+      const float *src = c.part + ((size_t)(it.x + min(s0 + kMergeGroups * i, it.y - 1) * it.z) * WAVES + wave) * kPartFloats<D>;
       ms[i] = src[64 * (D / 2) + lane];
       ls[i] = src[64 * (D / 2) + 64 + lane];
       const f32x4_t *o4 = reinterpret_cast<const f32x4_t *>(src) + 4 * 64 * dt + lane;
@@ -877,37 +877,49 @@ struct Division {
   int whole, tail;  // (kTail) tiles that are not divided, parts of each other
   long long slots() const { return mode == kParts ? (long long)rounds * kPlaces : mode == kTail ? slots_tail : 0; }
   long long slots_tail;
+  float cost = 0.f;  // (the last round's tiles) rounds that all take
 };
 // Fewer tiles than places: all are divided, but of one sequence only where that gives three parts in two rounds.  Up to
 // kTailRounds rounds: the r tiles of the last one, into as many parts (8 at most, 1024 in all) as let it end soonest, a part
 // costing 0.03 of a whole tile beside its keys.  us whole -> divided, 4680 queries, 32760 keys: 4 heads of 37 tiles 534 -> 330, 8
 // (296 tiles) 763 -> 637, 14 (518) 1375 -> 1010, 16 (592) 1389 -> 1169, 18 1445 -> 1320, 32 2352 -> 2252; 9360 keys, 16 heads, 334 -> 300.
 constexpr int kTailRounds = 8, kBrief = 80 * kStage;
+static Division divide_last(long long n_items, int places) {
+  const int r = (int)(n_items % places);
+  const float before = (float)(n_items / places);
+  if (n_items < places || n_items > (long long)kTailRounds * places || r == 0) return {kWhole, 1, 0, 1, 0, before + (r ? 1.f : 0.f)};
+  int best = 1;
+  float least = 1e9f;
+  for (int p = 1; p <= 8 && r * p <= 2 * places; ++p) {
+    const float cost = (float)((r * p + places - 1) / places) / p + (p > 1 ? 0.03f * p * r / places + 0.02f : 0.f);
+    if (cost < least) least = cost, best = p;
+  }
+  if (best == 1) return {kWhole, 1, 0, 1, 0, before + 1.f};
+  return {kTail, 1, (int)n_items - r, best, (long long)r * best, before + least};
+}
 static Division divide(int B, long long n_items) {
   if (n_items < kPlaces && B <= kSplitSeqs && (B > 1 || 3 * n_items <= 2 * kPlaces))
     return {kParts, 3 * n_items > kPlaces ? 2 : 1, 0, 1, 0};
-  const int r = (int)(n_items % kPlaces);
-  if (n_items < kPlaces || n_items > kTailRounds * kPlaces || r == 0) return {kWhole, 1, 0, 1, 0};
-  int best = 1;
-  float least = 1e9f;
-  for (int p = 1; p <= 8 && r * p <= 2 * kPlaces; ++p) {
-    const float cost = (float)((r * p + kPlaces - 1) / kPlaces) / p + (p > 1 ? 0.03f * p * r / kPlaces + 0.02f : 0.f);
-    if (cost < least) least = cost, best = p;
-  }
-  if (best == 1) return {kWhole, 1, 0, 1, 0};
-  return {kTail, 1, (int)n_items - r, best, (long long)r * best};
+  return divide_last(n_items, kPlaces);
 }
 
 // int8, D = 128: tiles of 256 rows, eight wavefronts, that share what it takes to turn codes into f16 (VALU instructions of a wavefront
-// and stage 274 -> 230).  They are not divided, so: where long sequences have four tiles each, on average, and the last round of
-// the chip's 256 places is full but for a seventh.  us of tiles of 128 and of 256, 4680 queries of 32760 keys: 40 heads (760 tiles)
-// 3366 / 2994, 24 (456) 2152 / 1895, 12 (228) 1076 / 974, but 16 (304) 1303 / 1819; six ragged prompts of up to 2048 tokens, 40 on 8
+// and stage 274 -> 230).  Where long sequences have four tiles each, on average, and the rounds of the chip's 256 places, the last one
+// divided if that pays, are full but for a seventh.  us of tiles of 128 and of 256, 4680 queries of 32760 keys: 40 heads (760 tiles)
+// 3366 / 2994, 24 (456) 2152 / 1895, 16 (304) 1266 / 1193, 12 (228) 1076 / 974, 8 (152) 772 / 869; six ragged prompts of up to 2048 tokens, 40 on 8
 // heads, 12000 keys 755 / 739; 4680 keys, 40 heads, 313 / 316; 64 of up to 256 tokens, 8 heads 135 / 149.
 constexpr int kWideTile = 256, kWidePlaces = 256;
-static bool wide_tiles(const heart_cache &c, int T, int Hq) {
-  if (c.type != HEART_CACHE_INT8 || c.D != 128 || (long long)c.max_pages * c.page <= kBrief) return false;
-  const long long tiles = most_items(kWideTile, c.B, c.H, T, Hq), round = (tiles + kWidePlaces - 1) / kWidePlaces * kWidePlaces;
-  return (long long)T * (Hq / c.H) >= 4ll * kWideTile * c.B && 7 * tiles >= 6 * round;
+static bool may_be_wide(int type, int B, int H, int D, int T, int Hq) {
+  return type == HEART_CACHE_INT8 && D == 128 && (long long)T * (Hq / H) >= 4ll * kWideTile * B;
+}
+static bool wide_tiles(const heart_cache &c, int T, int Hq, bool divided, Division &d) {
+  if (!may_be_wide(c.type, c.B, c.H, c.D, T, Hq) || (long long)c.max_pages * c.page <= kBrief) return false;
+  const long long tiles = most_items(kWideTile, c.B, c.H, T, Hq);
+  Division w = divide_last(tiles, kWidePlaces);
+  if (!divided) w = {kWhole, 1, 0, 1, 0, (float)((tiles + kWidePlaces - 1) / kWidePlaces)};
+  if (7.f * (float)tiles < 6.f * kWidePlaces * w.cost) return false;
+  d = w;
+  return true;
 }
 
 size_t cache_attn_workspace_bytes(int type, int B, int H, int D, int T, int Hq) {
@@ -917,6 +929,11 @@ size_t cache_attn_workspace_bytes(int type, int B, int H, int D, int T, int Hq) 
   const size_t part = D == 128 ? kPartFloats<128> : kPartFloats<64>;
   const size_t many = d.mode == kWhole ? 0 : kPlaces * sizeof(int4) + (size_t)d.slots() * 4 * part * sizeof(float);
   // (which kernel it is goes by the page tables' room too, which is not known here)
+  if (may_be_wide(type, B, H, D, T, Hq)) {
+    const Division w = divide_last(most_items(kWideTile, B, H, T, Hq), kWidePlaces);
+    const size_t wide = w.mode == kWhole ? 0 : kPlaces * sizeof(int4) + (size_t)w.slots() * (kWideTile / 32) * part * sizeof(float);
+    return wide > many ? wide : many;
+  }
   return type == HEART_CACHE_INT8 && (long long)T * (Hq / H) <= (long long)kIntRows * B && few > many ? few : many;
 }
 
@@ -936,7 +953,14 @@ static int launch_t(const AttnCall &c, const Division &d, bool wide, hipStream_t
   };
   auto run = [&](auto mode, long long grid) -> int { return run_waves(mode, grid, std::integral_constant<int, kTile / 32>{}); };
   if constexpr (kKind == kInt8 && D == 128)
-    if (wide) return run_waves(std::integral_constant<CacheMode, kWhole>{}, c.n_items, std::integral_constant<int, kWideTile / 32>{});
+    if (wide) {
+      constexpr int W = kWideTile / 32;
+      const std::integral_constant<int, W> waves{};
+      if (d.mode == kWhole) return run_waves(std::integral_constant<CacheMode, kWhole>{}, c.n_items, waves);
+      if (int rc = run_waves(std::integral_constant<CacheMode, kTail>{}, c.whole + d.slots(), waves)) return rc;
+      hipLaunchKernelGGL((cache_attn_merge_kernel<D, kTail, W>), dim3((unsigned)((c.n_items - c.whole) * W)), dim3(D * 2 * kMergeGroups), 0, st, c);
+      return check_launch("cache_attn_merge_kernel");
+    }
   if (d.mode == kWhole) return run(std::integral_constant<CacheMode, kWhole>{}, c.n_items);
   if (d.mode == kParts) {
     const int rc = c.s.B <= 64 ? run(std::integral_constant<CacheMode, kParts>{}, d.slots())
@@ -978,7 +1002,7 @@ int launch_cache_attn(const heart_cache &c, int T, int Hq, const void *q, const 
     d.rounds = 1;
   }
   if (!workspace) d = {kWhole, 1, 0, 1, 0};
-  const bool wide = wide_tiles(c, T, Hq);
+  const bool wide = wide_tiles(c, T, Hq, workspace != nullptr, d);
   a.n_items = (int)(wide ? most_items(kWideTile, c.B, c.H, T, Hq) : items);
   a.rounds = d.rounds;
   a.whole = d.whole;

@@ -54,6 +54,9 @@ def test_workspace_of_attention(lib):  # noqa: F811
         few = size(B, 2, B=B)
         assert size(T, Hq, B=B, **int8) == max(few, size(T, Hq, B=B)) >= few > 0
     assert size(300 * 20, 2, B=300, **int8) == size(300 * 20, 2, B=300)  # (more sequences than are divided)
+    # tiles of 128 rows, and of 256 whose last round is divided
+    assert size(1024, 60, B=1, H=60, **int8) > size(1024, 60, B=1, H=60) and size(1024, 60, B=1, H=60, D=64, **int8) == size(1024, 60, B=1, H=60, D=64)
+    assert size(4680, 12, B=1, H=12, **int8) == size(4680, 12, B=1, H=12)
 
 
 def test_binding_asks_for_the_workspace_of_the_type(lib):  # noqa: F811

@@ -257,6 +257,34 @@ def test_wide_tiles(B, n, kvs, G, page, causal, window):
         assert_near(lse[0][h:h + 1], want_lse, ltol, "lse")
 
 
+@pytest.mark.parametrize("H,n,kv,causal,window", [(60, 1100, 4200, 1, 0), (60, 1030, 4199, 500, 3000), (55, 1281, 2600, 0, 0)])
+def test_wide_tiles_of_a_divided_round(H, n, kv, causal, window):
+    """300 and 330 tiles of 256 rows: those of the last round are divided and added up, the others have the bits that they have
+    undivided."""
+    D = 128
+    c = Blocks([kv], H, D, 64, seed=n, room=5200, spread=5)
+    q = new_q(n, H, D)
+    need = heart.heart_cache_attn_workspace_bytes(q, c.stored["k"], c.page_table)
+    assert need > 0
+    got = []
+    for ws in (torch.full((need,), 0x55, dtype=torch.uint8, device="cuda"), None):
+        print(f"cache_attn int8 wide, last round H={H} n={n} kv={kv} causal={causal} window={window} workspace={ws is not None}", flush=True)
+        lse = torch.zeros((H, n), device="cuda")
+        got.append((heart.heart_cache_attn(q.cuda(), *c.args(), causal=causal, window=window, lse=lse, workspace=ws, **c.scale_args()), lse))
+        torch.cuda.synchronize()
+    differ = (got[0][0] != got[1][0]).any(-1).float().mean().item()
+    assert 0 < differ < 0.5
+    one = Blocks([kv], 1, D, 64, seed=n, room=5200, device="cpu")
+    one.table_cpu = c.table_cpu
+    for h in (0, H // 2, H - 1):
+        for w in ("k", "v"):
+            one.codes[w], one.scales[w] = c.codes[w][:, h:h + 1], c.scales[w][:, h:h + 1]
+        want, want_lse, tol, ltol = tolerance(one, q[:, h:h + 1], [n], causal, window)
+        for out, lse in got:
+            assert_near(out[:, h:h + 1], want, tol, "out")
+            assert_near(lse[h:h + 1], want_lse, ltol, "lse")
+
+
 def test_wide_tiles_of_anything():
     """Ragged ranges, pages that are none, a scale that is NaN and lengths that are none, of tiles of 256 rows."""
     H, D, kvs, qs = 16, 128, [1300, 1100, 0], [1290, 1100, 700]
