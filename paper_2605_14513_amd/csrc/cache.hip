@@ -8,7 +8,8 @@
 // three or four lane exchanges on the VALU.
 //
 // us: reading 32760 tokens of 12 heads of 128 from e4m3 (303 MB in and out) 60 (5.1 TB/s, a copy of 512 MB 4.7), of 40 heads 189;
-// writing 4680 tokens of 40 heads and reading them back 62; the tokens of 64 sequences 4.5.  Stores past the caches make the
+// writing 4680 tokens of 40 heads and reading them back 62; the tokens of 64 sequences 4.5.  From int8 the same, 61 and 46 (9360
+// tokens of 40 heads, 288 MB, just written).  Stores past the caches make the
 // first 53, but the pooling that reads what was read back then takes 36 instead of 23.
 #include <type_traits>
 

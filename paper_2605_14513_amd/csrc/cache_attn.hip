@@ -26,10 +26,14 @@
 //   e4m3: the codes are loaded into registers a stage earlier still and written to LDS as the bf16 values that they
 //     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
 //     time than the products take.
+//   int8: the same, as f16, which a code becomes in one instruction (bf16 would take one and a half), with f16 products: K as the codes
+//     are, its scales, of 16 rows each, as factors of the logits; V times its scale by a power of two of the part; Q by its
+//     row's power of two.  Weights in f16 have 11 bits, and the largest of a row is 2^7 at least, which keeps small ones from f16's
+//     least.  Eight wavefronts share a stage's conversion where tiles of 256 rows fill the chip (wide_tiles).
 //
 // Bound by the matrix instructions and the power that they draw.  PFLOP/s: 4680 queries of 12 heads over 32760 keys in bf16
 // 1.03 to 1.07 (matrix pipes busy 59 % of the cycles), of 40 heads in e4m3 0.99 to 1.04 (53 %: the conversions); a bf16 matrix
-// product of 8192^3 1.20.  Calls of few tiles are bound by latency: 16 sequences with 8 drafts of 24 heads, window 4096, 20 us.
+// product of 8192^3 1.20; of 40 heads in int8 1.01 to 1.05 (53 %; tiles of 128 rows 0.91 to 0.95).  Calls of few tiles are bound by latency: 16 sequences with 8 drafts of 24 heads, window 4096, 20 us.
 #include <type_traits>
 
 #include "cache_attn_device.h"
@@ -904,7 +908,7 @@ static Division divide(int B, long long n_items) {
 }
 
 // int8, D = 128: tiles of 256 rows, eight wavefronts, that share what it takes to turn codes into f16 (VALU instructions of a wavefront
-// and stage 274 -> 230).  Where long sequences have four tiles each, on average, and the rounds of the chip's 256 places, the last one
+// and stage 274 -> 234).  Where long sequences have four tiles each, on average, and the rounds of the chip's 256 places, the last one
 // divided if that pays, are full but for a seventh.  us of tiles of 128 and of 256, 4680 queries of 32760 keys: 40 heads (760 tiles)
 // 3366 / 2994, 24 (456) 2152 / 1895, 16 (304) 1266 / 1193, 12 (228) 1076 / 974, 8 (152) 772 / 869; six ragged prompts of up to 2048 tokens, 40 on 8
 // heads, 12000 keys 755 / 739; 4680 keys, 40 heads, 313 / 316; 64 of up to 256 tokens, 8 heads 135 / 149.

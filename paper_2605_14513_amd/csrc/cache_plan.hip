@@ -1,12 +1,13 @@
 // heart_cache_plan: pages, token ranges, slots and positions of a step's new tokens, from the requests' lengths.
 //
 // Five prefix sums over the requests say all: pages that go back, pages asked for, tokens of those whose pages are there, and
-// pages and tokens of those that are granted.  One workgroup computes them, in three rounds (sums saturate: lengths may be
+// pages and tokens of those that are granted.  A workgroup computes them in three rounds (sums saturate: lengths may be
 // anything).  What they place -- pages back on the list, pages from it into the table, a slot and a position for each token -- is
 // independent, each item found by a search in the sums.
 //
 // Bound by latency: chains of loads, each of which takes a microsecond where another XCD wrote what it reads, and launches.  So
-// sums that are searched lie in LDS, and there are as few launches as can be (struct PlanMode).
+// sums that are searched lie in LDS, and there are as few launches as can be (enum PlanMode).  us: three requests 4.5, 256 with drafts
+// 6.8, 1500 with 655 K tokens (8 MB out) 13.8, 25 with three launches that search in memory.
 #include <algorithm>
 
 #include "heart_internal.h"
