@@ -169,7 +169,7 @@ struct Work {
 inline long long most_items(int tile, int B, int H, int T, int Hq) { return ((long long)T * (Hq / H) / tile + B) * H; }
 
 // Few rows a key head (cache_attn_few.hip).
-constexpr int kIntRows = 64;  // (int8) rows a sequence and key head, on average, at most
+constexpr int kIntRows = 512;  // (int8) rows a sequence and key head, on average, at most
 bool cache_attn_few(int B, int H, int T, int Hq);
 bool cache_attn_int8_few(const heart_cache &c, int T, int Hq);
 size_t cache_attn_few_workspace_bytes(int B, int H, int D, int T, int Hq);

@@ -751,7 +751,8 @@ bool cache_attn_few(int B, int H, int T, int Hq) { return (long long)T * (Hq / H
 // The same where tiles have little to read, of int8 (keys: what the page tables have room for): tiles at most, all in one round of
 // places, their keys together, and of one.  us of this kernel and of the other, D = 128: 24 rows, 8 heads of 1000 keys 12.6 / 18.8, of
 // 4000 17.1 / 20.4, 16 sequences 23.1 / 28.9 and 53.8 / 46.3; 64 rows, 8 heads of 300 keys 12.4 / 15.9, of 4000 20.7 / 20.8, 16 sequences
-// 18.0 / 25.3 and 91.9 / 54.8; 64 sequences, 24 rows, 300 keys 25.6 / 21.1; 64 rows, two heads of 16000 keys 35.5 / 28.4.
+// 18.0 / 25.3 and 91.9 / 54.8; 64 sequences, 24 rows, 300 keys 25.6 / 21.1; 64 rows, two heads of 16000 keys 35.5 / 28.4; 256 rows, 8 heads
+// of 300 keys 8.8 / 17.0, of 1500 20.1 / 22.5; 500 rows, 8 heads of 700 keys 17.4 / 21.1.
 constexpr long long kIntTiles = 640, kIntKeys = 5 << 16, kIntLongest = 4096;
 bool cache_attn_int8_few(const heart_cache &c, int T, int Hq) {
   if (cache_attn_few(c.B, c.H, T, Hq)) return true;

@@ -222,7 +222,8 @@ def test_columns_that_the_weights_cancel(D, n):
 def test_either_kernel_around_its_limits(D):
     """Rows, tiles and keys on either side of what the kernel for few rows takes of int8 (tables with room for just so many)."""
     for B, n, kv, H, G, room in ((1, 64, 700, 2, 1, 0), (1, 65, 700, 2, 1, 0), (2, 16, 4096, 1, 4, 4096), (2, 16, 4096, 1, 4, 4097),
-                                 (2, 4, 600, 2, 5, 0), (20, 16, 300, 8, 4, 0), (64, 16, 200, 2, 4, 0), (65, 16, 200, 2, 4, 0), (3, 17, 48, 1, 1, 0)):
+                                 (2, 4, 600, 2, 5, 0), (20, 16, 300, 8, 4, 0), (64, 16, 200, 2, 4, 0), (65, 16, 200, 2, 4, 0), (3, 17, 48, 1, 1, 0), (1, 512, 700, 2, 1, 0),
+                                 (1, 513, 700, 2, 1, 0), (2, 100, 130, 3, 5, 0), (1, 300, 1024, 2, 1, 1024)):
         c = Blocks([max(n, kv - 11 * b) for b in range(B)], H, D, 16, seed=n, room=room)
         for ws in ("auto", None):
             check(c, new_q(B * n, H * G, D), [n] * B, cu=B % 2 == 0, workspace=ws)

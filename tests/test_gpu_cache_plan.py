@@ -201,7 +201,7 @@ def test_refused_tensors():
             call(a)
     for kw, error, text in ((dict(keep=i32([0])), ValueError, "keep"), (dict(cu_q=i32([0] * 3)), ValueError, "cu_q"),
                             (dict(slots=i32([0] * 5)), TypeError, "int64"), (dict(positions=torch.zeros(5, device="cuda")), TypeError, "int32"),
-                            (dict(n=-1, slots=None), (ValueError, RuntimeError), "")):
+                            (dict(n=-1, slots=None), (ValueError, RuntimeError), "negative")):
         with pytest.raises(error, match=text):
             call(s, **kw)
     with pytest.raises(heart.HeartError, match="workspace"):
