@@ -383,7 +383,7 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * a key head or less on average, to a sum of two bf16.  Cached rows of 8 bits enter as the bf16 values they stand for (as part
  * of the weights, v's exponents, where these are two bf16: below an exponent of 32 they lose bits).  Of int8 the codes are
  * multiplied and the scales applied in fp32 where a sequence has 16 rows or less (512, where there is little to be read) and weights
- * are two bf16; else products are of f16: queries by their row's power of two (elements below 2^-32 of the largest lose bits), k's
+ * are two bf16; else products are of f16: queries by their row's power of two (elements below 2^-31 of the largest lose bits), k's
  * codes, v's values by a power of two of the tile (those under scales below 2^-26 of its largest lose bits), weights rounded to
  * f16 (below 2^-21 of the largest they lose bits).  Rows from kv_len on may
  * hold anything, pages of nobody too; a NaN or an infinity among the first kv_len tokens (int8: a scale that is one) may also

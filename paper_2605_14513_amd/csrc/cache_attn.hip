@@ -465,7 +465,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const u32x4_t *>(src + ks * 16);
   }
-  // (int8) Q in f16, with its row's power of two outside: exact but for elements below 2^-32 of the row's largest
+  // (int8) Q in f16, with its row's power of two outside: exact but for elements below 2^-31 of the row's largest
   float row_unit = scale_log2e;  // logits in log2 units are this times K's scale times the accumulator
   if constexpr (kInts) {
     uint32_t top = 0, sw0, sw1;

@@ -81,7 +81,7 @@ def test_order_of_refusals(B):
     assert s["kv_len"][:5].tolist() == [21, 21, 16, 16, 16]
 
 
-@pytest.mark.parametrize("B,T", [(7, 50), (1100, 4000), (7, 20000)])
+@pytest.mark.parametrize("B,T", [(7, 50), (1100, 4000), (7, 20000), (4200, 3000)])
 def test_arrays_that_hold_anything(B, T):
     """Lengths, lists and tables of no sense: as the definition, and nothing outside the arrays is touched."""
     page, M, n_pages = 16, 6, 40
@@ -121,7 +121,7 @@ def test_arrays_that_hold_anything(B, T):
 
 
 def test_keep_may_be_the_lengths():
-    for B in (9, 1100):
+    for B in (9, 1100, 4200):
         r = random.Random(B)
         kv, table, free, n_free = state(B, 8, 16, r, 5 * B)
         add = [r.randint(0, 3) for _ in range(B)]
@@ -149,7 +149,7 @@ def test_outputs_that_are_not_asked_for():
         assert cu.tolist() == want["cu_q"] and s[1].tolist() == want["page_table"] and s[3].item() == want["n_free"][0]
 
 
-@pytest.mark.parametrize("B,T", [(6, 60), (1100, 5000)])
+@pytest.mark.parametrize("B,T", [(6, 60), (1100, 5000), (4200, 9000)])
 def test_captured_plans_follow_the_lengths(B, T):
     """A plan captured once and replayed: lengths, additions and refusals of every replay are those that are there then, with
     eager plans on the same workspace in between."""
