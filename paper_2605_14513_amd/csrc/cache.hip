@@ -8,7 +8,7 @@
 // three or four lane exchanges on the VALU.
 //
 // us: reading 32760 tokens of 12 heads of 128 from e4m3 (303 MB in and out) 60 (5.1 TB/s, a copy of 512 MB 4.7), of 40 heads 189;
-// writing 4680 tokens of 40 heads and reading them back 62; the tokens of 64 sequences 4.5.  From int8 the same, 61 and 46 (9360
+// writing 4680 tokens of 40 heads and reading them back 62; the tokens of 64 sequences 4.5.  From int8 57, and 46 (9360
 // tokens of 40 heads, 288 MB, just written).  Stores past the caches make the
 // first 53, but the pooling that reads what was read back then takes 36 instead of 23.
 #include <type_traits>
@@ -157,7 +157,8 @@ struct CacheOut {  // K or V
   long long db, dh, dt;  // batch, head, token (bf16 elements)
 };
 
-template <int D, CacheKind kKind>
+// kOnce: codes are loaded past the caches
+template <int D, CacheKind kKind, bool kOnce = false>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheOut k, CacheOut v, CacheSeqs s, int H, int N, int tiles) {
   constexpr int LPR = D / 8, RPI = 64 / LPR, NI = kRowsWave / RPI;
   constexpr bool kCodes = kKind != kBf16;
@@ -182,7 +183,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheOut k, CacheOut v,
     for (int i = 0; i < NI; ++i) {
       const int o = o0 + i * RPI + sub;
       if constexpr (kCodes) {
-        const u32x2_c y = *reinterpret_cast<const u32x2_c *>(src + o * c.st + col * 8);
+        const u32x2_c *from = reinterpret_cast<const u32x2_c *>(src + o * c.st + col * 8);
+        const u32x2_c y = kOnce ? __builtin_nontemporal_load(from) : *from;
         x[side][i] = u32x4_c{y.x, y.y, 0, 0};
         if constexpr (kKind == kE4m3) byte[side][i] = exp[o];
       } else {
@@ -248,7 +250,14 @@ int launch_cache_read(const heart_cache &c, int N, void *k, const long long ks[3
   };
   auto of_kind = [&](auto d) -> int {
     constexpr int D = decltype(d)::value;
-    if (c.type == HEART_CACHE_INT8) return run(cache_read_kernel<D, kInt8>);
+    if (c.type == HEART_CACHE_INT8) {
+      // Codes of calls that read a lot, by their room, would be gone from the memory-side cache (256 MB) before anybody reads them
+      // again, for twice as many bytes are stored.  us with and without: 32760 tokens of 12 heads (100 MB) 57.1 / 60.4, just
+      // written ones of 40 heads (96 MB) alike; of less they stay: 64 sequences of up to 500 tokens, read again and again, 30.4 / 25.6.
+      constexpr long long kOnceFrom = 80ll << 20;
+      const long long rows = (long long)c.B * c.H * (N < cap ? N : cap);
+      return rows > kOnceFrom / (2 * D) ? run(cache_read_kernel<D, kInt8, true>) : run(cache_read_kernel<D, kInt8>);
+    }
     return c.type == HEART_CACHE_E4M3 ? run(cache_read_kernel<D, kE4m3>) : run(cache_read_kernel<D, kBf16>);
   };
   return c.D == 128 ? of_kind(std::integral_constant<int, 128>{}) : of_kind(std::integral_constant<int, 64>{});

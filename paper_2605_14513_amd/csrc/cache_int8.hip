@@ -10,8 +10,8 @@
 // large enough; else their codes are divided anew, which is the only case that reads them.  The jobs of a sequence start at the
 // number  first / page + 2 b  (n tokens are in n / page + 2 pages at most), which every wavefront inverts on its own.
 //
-// Bound by memory, by latency where there are few tokens.  4680 tokens of 40 heads of 128 (144 MB in and out) 31 to 36 us, 4.0 to 4.6 TB/s (a
-// copy of 512 MB 5.2), with one, two or four wavefronts for a page of 64 tokens alike; one token of each of 64 sequences 4.5.
+// Bound by memory, by latency where there are few tokens.  4680 tokens of 40 heads of 128 (144 MB in and out) 27 us, 5.3 TB/s (as a copy of
+// 512 MB), with one, two or four wavefronts for a page of 64 tokens alike; one token of each of 64 sequences 4.5.
 #include <type_traits>
 
 #include "cache_device.h"
@@ -95,7 +95,9 @@ __global__ __launch_bounds__(256) void cache_write_blocks_kernel(BlockSide k, Bl
   for (int i = 0; i < NI; ++i) {
     const int r = r0 + i * RPI + sub;
     x[i] = u32x4_c{0, 0, 0, 0};
-    if (r >= o0 && r < o1) x[i] = *reinterpret_cast<const u32x4_c *>(src + r * c.st);
+    // (past the caches: these rows are read once, the codes that are stored here are read next.  4680 tokens of 40 heads written and
+    // 9360 read back 82.7 us, 87.3 without)
+    if (r >= o0 && r < o1) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_c *>(src + r * c.st));
   }
   if (page < 0) return;  // (here, so that rows are on their way meanwhile)
   float *scale_at = c.scale + ((long long)page * H + h);

@@ -153,6 +153,20 @@ def test_ranges_that_fall_or_leave_the_tensors():
             assert (c.scale[n][~named].isnan()).all()
 
 
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 256)])
+def test_reading_much(D, page):
+    """More codes than are read through the caches, by the room of the outputs."""
+    H, N = 33, 2 * (81 << 20) // (2 * 33 * D * 2) + 5
+    c = Blocks([700, 0], H, D, page, seed=D, room=N)
+    k, v = (torch.full((2, H, N, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    print(f"cache_read int8 of room for {N} tokens, H={H} D={D}", flush=True)
+    heart.heart_cache_read(*c.args(), k=k, v=v, **c.scale_args())
+    torch.cuda.synchronize()
+    for name, got in (("k", k), ("v", v)):
+        assert torch.equal(got[0, :, :700].cpu(), c.sequence(name, 0).float().bfloat16())
+        assert (got[0, :, 700:] == 7.0).all() and (got[1] == 7.0).all()
+
+
 def test_no_tokens():
     c = Blocks([5, 0], 1, 64, 16, seed=1)
     x = torch.zeros((0, 1, 64), dtype=torch.bfloat16, device="cuda")
