@@ -10,8 +10,8 @@
 // large enough; else their codes are divided anew, which is the only case that reads them.  The jobs of a sequence start at the
 // number  first / page + 2 b  (n tokens are in n / page + 2 pages at most), which every wavefront inverts on its own.
 //
-// Bound by memory, by latency where there are few tokens.  4680 tokens of 40 heads of 128 (144 MB in and out) 27 us, 5.3 TB/s (as a copy of
-// 512 MB), with one, two or four wavefronts for a page of 64 tokens alike; one token of each of 64 sequences 4.5.
+// Bound by memory, by latency where there are few tokens.  4680 tokens of 40 heads of 128 (144 MB in and out) 27 us, 5.3 TB/s (as a
+// copy of 512 MB), with one, two or four wavefronts for a page of 64 tokens alike; one token of each of 64 sequences 4.5.
 #include <type_traits>
 
 #include "cache_device.h"
