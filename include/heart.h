@@ -323,8 +323,7 @@ size_t heart_attn_balanced_workspace_bytes(const heart_shape *shape, int dense);
  *   HEART_CACHE_INT8: elements are signed 8-bit whole numbers, and k_exp, v_exp point to float [n_pages,H] (contiguous,
  *     16-byte aligned), a scale for each page and head: an element stands for code * scale.  For rows of about one size
  *     (normalised keys) the error of writing is 2/5 of that of e4m3, for rows of very different sizes in a page it is larger.
- *     heart_cache_write gives scales of 3 significant bits; other positive ones may be read and attended to, those of v with
- *     up to 7 significant bits.
+ *     heart_cache_write gives scales of 3 significant bits; other positive ones may be read and attended to.
  * B sequences: page_table int32 [B,max_pages] names the pages of each in order, kv_len int32 [B] says how many tokens it
  * has, the T new tokens of the call among them; all DEVICE memory, read when the call runs, so a captured call follows what
  * they hold at each replay.  cu_q int32 [B+1] or NULL: the new tokens of sequence b are tokens cu_q[b] .. cu_q[b+1]-1 of the
@@ -384,8 +383,9 @@ int heart_cache_read(const heart_cache *cache, int N, void *k, const long long k
  * of the weights, v's exponents, where these are two bf16: below an exponent of 32 they lose bits).  Of int8 the codes are
  * multiplied and the scales applied in fp32 where a sequence has 16 rows or less (512, where there is little to be read) and weights
  * are two bf16; else products are of f16: queries by their row's power of two (elements below 2^-31 of the largest lose bits), k's
- * codes, v's values by a power of two of the tile (those under scales below 2^-26 of its largest lose bits), weights rounded to
- * f16 (below 2^-21 of the largest they lose bits).  Rows from kv_len on may
+ * codes, v's values by a power of two of the tile (its scales are rounded to f16's 11 bits, and products of more bits with codes once
+ * more; those under scales below 2^-26 of its largest, of more bits than 3 below 2^-19, lose bits), weights rounded to f16 (below
+ * 2^-21 of the largest they lose bits).  Rows from kv_len on may
  * hold anything, pages of nobody too; a NaN or an infinity among the first kv_len tokens (int8: a scale that is one) may also
  * reach queries that do not see it.  (Weights are up to 2^8, of int8 2^15, before the division by their sum: that times sum |v|
  * over a query's keys has to stay below 2^128, and v's exponents below 247.)  out must not overlap q.  T Hq is at most 2^30.

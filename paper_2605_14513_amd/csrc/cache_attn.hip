@@ -27,7 +27,8 @@
 //     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
 //     time than the products take.
 //   int8: the same, as f16, which a code becomes in one instruction (bf16 would take one and a half), with f16 products: K as the codes
-//     are, its scales, of 16 rows each, as factors of the logits; V times its scale by a power of two of the part; Q by its
+//     are, its scales, of 16 rows each, as factors of the logits; V times its scale (of 11 bits; exact for those that are written
+//     here) by a power of two of the part, half an instruction more; Q by its
 //     row's power of two.  Weights in f16 have 11 bits, and the largest of a row is 2^7 at least, which keeps small ones from f16's
 //     least.  Eight wavefronts share a stage's conversion where tiles of 256 rows fill the chip (wide_tiles).
 //
@@ -162,7 +163,8 @@ __device__ __forceinline__ void item_at(const AttnCall &c, int i, int n_items, i
 }
 
 // (int8) Codes in a quarter of the bytes of w as f16, exactly: with the sign bit turned, the byte below 0x64 is 1024 + 128 + code.
-// Two of them, from byte 2 kUpper on: less 1152, or times `unit` less 1152 `unit` (exact for units of up to 7 significant bits).
+// Two of them, from byte 2 kUpper on; less 1152 they are the codes, before anything multiplies them: 1152 times a scale has no room
+// in f16 for scales of more than 7 significant bits, and what it lost would be added to all elements of a page alike.
 template <bool kUpper>
 __device__ __forceinline__ f16x2_t codes_up(uint32_t turned) {
   return __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, turned, kUpper ? 0x04030402u : 0x04010400u));
@@ -350,8 +352,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
   // codes: a stage in registers, written to LDS as 16-bit values
   u32x4_t raw[2][CPW];
   uint32_t raw_exp[2][CPW];
-  float raw_unit[2];      // (int8) of the wavefront's rows
-  f16x2_t v_mul, v_less;  // (int8) V's scale in units of v_unit, and what its codes are too large by, of the stage that is stored
+  float raw_unit[2];  // (int8) of the wavefront's rows
+  f16x2_t v_mul;      // (int8) V's scale in units of v_unit, of the stage that is stored
   const int crow = lane / LPC, cchunk = lane % LPC;
   auto load_codes = [&](int is_v, int i) __attribute__((always_inline)) {
     const uint32_t stride = is_v ? c.v.row : c.k.row;
@@ -400,18 +402,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
     if constexpr (kInts) {
       // K as the codes are (its scales go into the logits), V times its scale
       if (is_v && ii == 0 && p == 0) {
-        const _Float16 u = (_Float16)(raw_unit[1] * to_v_unit), less = (_Float16)-1152.f * u;
+        const _Float16 u = (_Float16)(raw_unit[1] * to_v_unit);
         v_mul = f16x2_t{u, u};
-        v_less = f16x2_t{less, less};
       }
-      const f16x2_t k_less = {(_Float16)-1152.f, (_Float16)-1152.f};
+      const f16x2_t less = {(_Float16)-1152.f, (_Float16)-1152.f};
       u32x4_t y;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         const uint32_t turned = x[2 * p + w] ^ 0x80808080u;
-        const f16x2_t a = codes_up<false>(turned), b = codes_up<true>(turned);
-        y[2 * w] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(a, v_mul, v_less) : a + k_less);
-        y[2 * w + 1] = __builtin_bit_cast(uint32_t, is_v ? __builtin_elementwise_fma(b, v_mul, v_less) : b + k_less);
+        const f16x2_t a = codes_up<false>(turned) + less, b = codes_up<true>(turned) + less;
+        y[2 * w] = __builtin_bit_cast(uint32_t, is_v ? a * v_mul : a);
+        y[2 * w + 1] = __builtin_bit_cast(uint32_t, is_v ? b * v_mul : b);
       }
       *reinterpret_cast<u32x4_t *>(dst + (((2 * cchunk + p) ^ f) * 16)) = y;
       // (where two wavefronts have 16 rows, the first's are there if any are)
