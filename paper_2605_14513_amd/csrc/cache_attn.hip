@@ -368,8 +368,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
       raw[is_v][ii] = __builtin_amdgcn_raw_buffer_load_b128(rs, (uint32_t)r * stride + (uint32_t)cchunk * 16u, 0, 0);
       if constexpr (kKind == kE4m3) raw_exp[is_v][ii] = __builtin_amdgcn_raw_buffer_load_b8(es, (uint32_t)r, 0, 0);
     }
+    // (K's without the sign that a NaN may have, for load_factors)
     if constexpr (kInts)
-      raw_unit[is_v] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(units[is_v]), i & 63));
+      raw_unit[is_v] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(units[is_v]), i & 63) & (is_v ? ~0u : 0x7fffffffu));
   };
   // (int8) V in f16 is in units of a power of two, 2^5 of which are above the largest scale of the part: known where the page ids
   // of its first stages are, of long parts after a look at the others
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
   constexpr int UC = 8 / DT;   // micro-ops of a C slot m < DT
   // (int8) what turns accumulators of the slice of position g into logits relative to the reference: factors of its two
   // groups of 16 keys, and the reference.  (Factors are no smaller than a normal number, so that -inf stays -inf; compared as
-  // whole numbers, so that a NaN stays one.)
+  // whole numbers, so that a positive NaN stays one.)
   float factor[2], less = 0.f;
   auto load_factors = [&](int g) __attribute__((always_inline)) {
     if constexpr (kInts) {

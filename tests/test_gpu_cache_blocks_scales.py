@@ -57,3 +57,30 @@ def test_scales_of_any_number_of_bits_in_tiles_of_256_rows(page, window):
             one.codes[w], one.scales[w] = c.codes[w][:, h:h + 1], c.scales[w][:, h:h + 1]
         want, _, tol, _ = tolerance(one, q[:, h:h + 1], [n], 1, window, weight=THREE)
         assert_near(out[:, h:h + 1], want, tol, "out")
+
+
+@pytest.mark.parametrize("bits", [0x7FC00000, -0x400000, 0x7F800001, -1])  # (quiet and signalling, of either sign)
+@pytest.mark.parametrize("n,room", [(1, 0), (20, 0), (150, 5200)])
+def test_a_scale_that_is_any_nan(n, room, bits):
+    """Queries that see the page get NaN, whatever NaN it is: 0 / 0 has its sign bit set on some machines."""
+    for D in (64, 128):
+        for w in ("k", "v"):
+            c = Blocks([600, 300], 2, D, 32, seed=n, room=room)
+            page = c.table_cpu[0, 3].item()  # (positions 96 to 127: all queries see it)
+            c.scale[w].view(torch.int32)[page, 1] = bits
+            print(f"cache_attn int8 NaN {bits:x} of {w} n={n} D={D} room={room}", flush=True)
+            lse = torch.zeros((4, 2 * n), device="cuda")
+            out = heart.heart_cache_attn(new_q(2 * n, 4, D).cuda(), *c.args(), lse=lse, **c.scale_args())
+            assert out[:n, 2:].isnan().all() and (w == "v" or lse[2:, :n].isnan().all())
+            assert not out[n:].isnan().any() and not out[:, :2].isnan().any() and not lse[:, n:].isnan().any()
+
+
+def test_a_scale_that_is_any_nan_in_tiles_of_256_rows():
+    H, n = 44, 1024
+    for bits in (0x7FC00000, -0x400000):
+        for w in ("k", "v"):
+            c = Blocks([1300], H, 128, 64, seed=1, room=5200)
+            c.scale[w].view(torch.int32)[c.table_cpu[0, 3].item(), 5] = bits
+            print(f"cache_attn int8 wide NaN {bits:x} of {w}", flush=True)
+            out = heart.heart_cache_attn(new_q(n, H, 128).cuda(), *c.args(), workspace=None, **c.scale_args())
+            assert out[:, 5].isnan().all() and not out[:, :5].isnan().any() and not out[:, 6:].isnan().any()
