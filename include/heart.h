@@ -358,7 +358,9 @@ typedef struct heart_cache {
  * and 127 s >= a, at least 2^-126; 0 for a = 0; NaN, which all of the page then reads as, where one of them is NaN or infinite.
  * A page whose first token is among the new ones gets s.  Another keeps its scale s0 if that is at least s (or NaN), else it
  * gets s, and the codes c of the rows before the new ones become round(c s0 / s).  A new element's code is round(x / scale), ties
- * to even.  Pages that new tokens are in must not be another sequence's too.
+ * to even.  Pages that new tokens are in must not be another sequence's too.  What a token did to its page's scale stays when the token is
+ * taken back (rejected drafts): codes stay as coarse as it made them, and the page NaN if it was not finite, until the page's first
+ * token is written anew.  (To have the page's other tokens back: take all of them back, and write them again.)
  */
 int heart_cache_write(const heart_cache *cache, int T, const void *k, const long long k_stride[2], const void *v,
                       const long long v_stride[2], const int *cu_q, void *stream);
@@ -406,7 +408,8 @@ size_t heart_cache_attn_workspace_bytes(const heart_cache *cache, int T, int Hq)
  * Plans a step: from the requests' lengths, which pages go back and which are taken, and where each new token is written.  Its
  * outputs are the arrays of the calls above; all is on the device, so the host need not know what was accepted or refused.
  * Of request b, in: kv_len[b] tokens in pages page_table[b][0 ..], keep[b] (NULL: all) of them stay (clamped to 0 .. kv_len[b];
- * 0: the request has ended, or begins anew), add[b] new ones are asked for (negative: 0).  First the pages that no kept token
+ * 0: the request has ended, or begins anew; of an int8 cache the others leave their pages' scales behind: heart_cache_write), add[b]
+ * new ones are asked for (negative: 0).  First the pages that no kept token
  * is in go back to the list, those of all requests; then requests are granted in order.  One is granted its add[b] tokens, all or
  * none, if kept and new tokens fit max_pages pages, if the list has pages for it and for all before it that fit the table (or if it
  * needs none: behind one that finds too few, only such are granted), and if the tokens of those that have their pages, up to

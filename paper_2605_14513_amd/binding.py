@@ -462,8 +462,8 @@ def heart_cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q=None, k_e
 
     k_cache, v_cache: [n_pages,H,page,D] views, bf16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages,H,page] (the rows'
     exponents), or int8 with k_scale, v_scale float32 [n_pages,H] (a scale for each page and head, which the call sets, or
-    raises where a page that has tokens gets larger ones: their codes are then divided anew); page_table int32
-    [B,max_pages]; kv_len int32 [B]: tokens of each sequence, the new ones among them; cu_q int32 [B+1]: where each sequence's
+    raises where a page that has tokens gets larger ones: their codes are then divided anew; tokens that are taken back, such
+    as rejected drafts, leave it as it is, also NaN, until the page's first token is written anew); page_table int32 [B,max_pages]; kv_len int32 [B]: tokens of each sequence, the new ones among them; cu_q int32 [B+1]: where each sequence's
     new tokens begin (None: T/B each)."""
     k_exp, v_exp = _units(k_cache, k_exp, v_exp, k_scale, v_scale)
     rc = _native().cache_write(k, v, k_cache, v_cache, page_table, kv_len, cu_q, k_exp, v_exp, torch._C._cuda_getDevice(),
