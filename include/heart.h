@@ -405,8 +405,9 @@ int heart_cache_attn(const heart_cache *cache, int T, int Hq, const void *q, con
 size_t heart_cache_attn_workspace_bytes(const heart_cache *cache, int T, int Hq);
 
 /*
- * Plans a step: from the requests' lengths, which pages go back and which are taken, and where each new token is written.  Its
- * outputs are the arrays of the calls above; all is on the device, so the host need not know what was accepted or refused.
+ * Plans a step: from the requests' lengths, which pages go back and which are taken, and where each new token is written.  Of its
+ * outputs the calls above take kv_len, page_table and cu_q; slots and positions are for a caller's own operators (position embeddings,
+ * rows beside the cache).  All is on the device, so the host need not know what was accepted or refused.
  * Of request b, in: kv_len[b] tokens in pages page_table[b][0 ..], keep[b] (NULL: all) of them stay (clamped to 0 .. kv_len[b];
  * 0: the request has ended, or begins anew; of an int8 cache the others leave their pages' scales behind: heart_cache_write), add[b]
  * new ones are asked for (negative: 0).  First the pages that no kept token

@@ -539,7 +539,9 @@ def heart_cache_plan_workspace_bytes(B: int, max_pages: int, n: int) -> int:
 def heart_cache_plan(add, kv_len, page_table, free_pages, n_free, page: int, n: Optional[int] = None, keep=None, cu_q=None,
                      slots=None, positions=None, workspace="auto"):
     """Plans a step on the GPU: which pages go back to the list, which requests get their new tokens, their pages, and where
-    each token is written.  Returns (cu_q int32 [B+1], slots int64 [n], positions int32 [n]) for the other calls on the cache.
+    each token is written.  Returns (cu_q int32 [B+1], slots int64 [n], positions int32 [n]): the other calls on the cache take
+    cu_q beside kv_len and page_table; slots (page * page size + row, -1 for none) and positions (-1 behind cu_q[B]) are for a
+    caller's own operators, and are made here in any case (the C call can leave them out).
 
     add int32 [B]: new tokens asked for; keep int32 [B] or None: cached tokens that stay (None: all; 0: the request has ended or
     begins anew).  Changed in place: kv_len int32 [B] (cached tokens of each, the new ones among them at the end), page_table

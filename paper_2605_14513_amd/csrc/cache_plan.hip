@@ -7,7 +7,9 @@
 //
 // Bound by latency: chains of loads, each of which takes a microsecond where another XCD wrote what it reads, and launches.  So
 // sums that are searched lie in LDS, and there are as few launches as can be (enum PlanMode).  us: three requests 4.5, 256 with drafts
-// 6.8, 1500 with 655 K tokens (8 MB out) 13.8, 25 with three launches that search in memory.
+// 6.8, 1500 with 655 K tokens (8 MB out) 13.8.  More than 4096 requests: three launches, the later two of which search in memory: 6000
+// with 654 K tokens 29 (4096 with as many, by two launches, 20), 6000 or 20000 with one token each 37 and 71, 20000 of which 200 or
+// three get one 92 and 173 (last_before_wave).
 #include <algorithm>
 
 #include "heart_internal.h"
@@ -25,7 +27,11 @@ constexpr int kPlanHeld = kPlanThreads * kPlanEach;  // requests that a workgrou
 constexpr int kPlanSumGroups = 64;   // most workgroups that sum
 constexpr int kPlanGroups = 2048;    // most workgroups of 256 threads that place items
 // New tokens that one workgroup places alone.  us alone, shared: 8 requests of 800 tokens 5.4, 9.1, of 8000 8.8, 9.0; 256 of 4096
-// 8.4, 10.6, of 8192 12.4, 11.0; 1000 of 4000 9.6, 12.2, of 8000 14.1, 12.6.  And places in the table, all of which may go back.
+// 8.4, 10.6, of 8192 12.4, 11.0; 1000 of 4000 9.6, 12.2, of 8000 14.1, 12.6.
+// And places in the table, all of which may go back, 1024 of them in a microsecond where one workgroup does it: 256 requests that get a
+// token each 7.0, 11.1, where 16 of them end, of 282 pages each, 11.7, 12.2; 1024 of which 90 end, of 120 pages, 23.6, 14.5; all
+// 2^18 pages at once 282, 15.  As many pages go back as are taken in the long run, a page a request in `page` tokens: so steps of
+// many are rare, and the bound is on what the rarest takes.
 constexpr int kPlanFew = 6000, kPlanFewPages = 1 << 18;
 
 struct PlanCall {
@@ -95,7 +101,9 @@ __device__ __forceinline__ int last_before(int lo, int hi, uint32_t x, F &&first
   return lo;
 }
 // The same for x0 + lane, of all B, by the whole wavefront: 64 places at a time for x0, then the 64 requests behind that one for
-// all lanes, and again 64 where that is not enough.  Few loads follow one another.
+// all lanes, and again 64 where that is not enough.  Few loads follow one another where most requests have items; where hardly any
+// have, one for each 64 of the requests up to the last lane's, and, as lanes behind the last item look for requests too, in that
+// item's wavefront up to the last request: 20000 of which three get a token take 173 us, where all get one 71.
 template <typename F>
 __device__ __forceinline__ int last_before_wave(int B, uint32_t x0, int lane, F &&first) {
   int lo = 0, n = B;
