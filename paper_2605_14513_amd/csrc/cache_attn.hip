@@ -1,8 +1,8 @@
 // heart_cache_attn: softmax attention of a chunk of new tokens over the paged key/value cache.
 //
 // Work.  The queries that share a key head (G query heads of each new token of a sequence) are rows of one product: row
-// r of sequence b and key head h is token r / G, query head h G + r % G.  A workgroup has a tile of 128 rows, a wavefront
-// 32 of them, and walks through the keys in stages of 64.
+// r of sequence b and key head h is token r / G, query head h G + r % G.  A workgroup has a tile of 128 rows
+// (some of int8 256), a wavefront 32 of them, and walks through the keys in stages of 64.
 //
 // Tiles are computed transposed, as in the block-sparse kernel, so that no accumulator moves between lanes:
 //   S^T (keys x rows) = K . Q^T,   O^T (d x rows) += V^T . P^T     with v_mfma_f32_32x32x16_bf16
@@ -18,13 +18,13 @@
 // maximum of slice s + 1.
 //
 // Stages.  K stage i holds slices 2i, 2i + 1; V stage i slices 2i - 1, 2i, so that one barrier per 64 keys retires both. Each
-// of the four wavefronts brings 16 rows of a stage, and pages hold a multiple of 16 tokens, so a wavefront needs one
+// of the four wavefronts brings 16 rows of a stage (of eight 8), and pages hold a multiple of 16 tokens, so a wavefront needs one
 // page for a stage: a buffer descriptor over the rows that are there (rows that no query of the tile sees, from kv_len on
 // in any case, and pages that the table does not name, are out of its range and arrive as zeros).  The page ids of 64
 // stages lie in one register, a lane each.
 //   bf16: LDS-direct loads, double-buffered, two slices ahead.
 //   e4m3: the codes are loaded into registers a stage earlier still and written to LDS as the bf16 values that they
-//     stand for, once for all four wavefronts; converting at each fragment read would be four times the work, more VALU
+//     stand for, once for all wavefronts; converting at each fragment read would be four times the work, more VALU
 //     time than the products take.
 //   int8: the same, as f16, which a code becomes in one instruction (bf16 would take one and a half), with f16 products: K as the codes
 //     are, its scales, of 16 rows each, as factors of the logits; V times its scale (of 11 bits; exact for those that are written
@@ -34,7 +34,9 @@
 //
 // Bound by the matrix instructions and the power that they draw.  PFLOP/s: 4680 queries of 12 heads over 32760 keys in bf16
 // 1.03 to 1.07 (matrix pipes busy 59 % of the cycles), of 40 heads in e4m3 0.99 to 1.04 (53 %: the conversions); a bf16 matrix
-// product of 8192^3 1.20; of 40 heads in int8 1.01 to 1.05 (53 %; tiles of 128 rows 0.91 to 0.95).  Calls of few tiles are bound by latency: 16 sequences with 8 drafts of 24 heads, window 4096, 20 us.
+// product of 8192^3 1.20; of 40 heads in int8 0.97 to 1.06 (53 %; tiles of 128 rows 0.91 to 0.95; D = 64, always of 128 rows, 0.79, where bf16
+// has 0.87).  Boxes differ by a tenth: on one box, in turn, bf16 1.10 to 1.14, e4m3 1.06, int8 1.05.  Calls of few tiles are bound by
+// latency: 16 sequences with 8 drafts of 24 heads, window 4096, 21 us.
 #include <type_traits>
 
 #include "cache_attn_device.h"
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
   }
 
   // ---- bringing K and V ----------------------------------------------------------------------
-  // The wavefront's 16 rows of stage i (of this part) are keys key0 + 64 i + 16 wave .. of K, 32 before that of V.
+  // The wavefront's ROWS rows of stage i (of this part) are keys key0 + 64 i + ROWS wave .. of K, 32 before that of V.
   // Page ids of stages base .. base + 63, lane l that of stage base + l.
   int ids[2];
   float units[2];  // (int8) their scales
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(const AttnCal
     }
   };
   const int in_page = (1 << c.s.page_shift) - 1;
-  // rows that are there of the wavefront's 16 of a stage, the address of the first one's element 0 and exponent
+  // rows that are there of the wavefront's ROWS of a stage, the address of the first one's element 0 and exponent
   auto rows_at = [&](int is_v, int i, uint64_t &addr, uint64_t &exp_addr) __attribute__((always_inline)) -> int {
     const CacheTensor &x = is_v ? c.v : c.k;
     const int key = key0 + i * kStage - 32 * is_v + ROWS * wave;
@@ -876,7 +878,8 @@ __global__ __launch_bounds__(D * 2 * kMergeGroups) void cache_attn_merge_kernel(
   }
 }
 
-// How the keys of a call of n_items tiles are divided: a function of that number alone.
+// How the keys of a call of n_items tiles are divided: by that number, that of the sequences and that of the places (of short sequences, by the
+// page tables' room, otherwise: launch_cache_attn).
 struct Division {
   CacheMode mode;
   int rounds;       // (kParts) of workgroups at most
@@ -886,7 +889,7 @@ struct Division {
   float cost = 0.f;  // (the last round's tiles) rounds that all take
 };
 // Fewer tiles than places: all are divided, but of one sequence only where that gives three parts in two rounds.  Up to
-// kTailRounds rounds: the r tiles of the last one, into as many parts (8 at most, 1024 in all) as let it end soonest, a part
+// kTailRounds rounds: the r tiles of the last one, into as many parts (8 at most, two for each place in all) as let it end soonest, a part
 // costing 0.03 of a whole tile beside its keys.  us whole -> divided, 4680 queries, 32760 keys: 4 heads of 37 tiles 534 -> 330, 8
 // (296 tiles) 763 -> 637, 14 (518) 1375 -> 1010, 16 (592) 1389 -> 1169, 18 1445 -> 1320, 32 2352 -> 2252; 9360 keys, 16 heads, 334 -> 300.
 constexpr int kTailRounds = 8, kBrief = 80 * kStage;
@@ -909,8 +912,8 @@ static Division divide(int B, long long n_items) {
   return divide_last(n_items, kPlaces);
 }
 
-// int8, D = 128: tiles of 256 rows, eight wavefronts, that share what it takes to turn codes into f16 (VALU instructions of a wavefront
-// and stage 274 -> 234).  Where long sequences have four tiles each, on average, and the rounds of the chip's 256 places, the last one
+// int8, D = 128: tiles of 256 rows, eight wavefronts, that share what it takes to turn codes into f16 (238 VALU instructions of a
+// wavefront and stage, some 40 fewer).  Where long sequences have four tiles each, on average, and the rounds of the chip's 256 places, the last one
 // divided if that pays, are full but for a seventh.  us of tiles of 128 and of 256, 4680 queries of 32760 keys: 40 heads (760 tiles)
 // 3366 / 2994, 24 (456) 2152 / 1895, 16 (304) 1266 / 1193, 12 (228) 1076 / 974, 8 (152) 772 / 869; six ragged prompts of up to 2048 tokens, 40 on 8
 // heads, 12000 keys 755 / 739; 4680 keys, 40 heads, 313 / 316; 64 of up to 256 tokens, 8 heads 135 / 149.

@@ -748,11 +748,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4 > 2 ? WAVES / 4 : 2) void cac
 // 4000 48.9 / 51.8, in e4m3 31.4 / 39.4, 64 of 1000 44.8 / 43.3, in e4m3 27.2 / 31.6; 24 rows (two tiles): 18 to 35 % slower
 // than that where one sequence is divided, 5 % faster to 9 % slower in batches.
 bool cache_attn_few(int B, int H, int T, int Hq) { return (long long)T * (Hq / H) <= (long long)kFewTile * B; }
-// The same where tiles have little to read, of int8 (keys: what the page tables have room for): tiles at most, all in one round of
-// places, their keys together, and of one.  us of this kernel and of the other, D = 128: 24 rows, 8 heads of 1000 keys 12.6 / 18.8, of
+// The same where tiles have little to read, of int8 (keys: what the page tables have room for, as lengths are not known here; one that has
+// room for more than these goes to the other kernel however short its sequences are): tiles at most (512 are one round of places), their
+// keys together, and of one.  us of this kernel and of the other, D = 128: 24 rows, 8 heads of 1000 keys 12.6 / 18.8, of
 // 4000 17.1 / 20.4, 16 sequences 23.1 / 28.9 and 53.8 / 46.3; 64 rows, 8 heads of 300 keys 12.4 / 15.9, of 4000 20.7 / 20.8, 16 sequences
 // 18.0 / 25.3 and 91.9 / 54.8; 64 sequences, 24 rows, 300 keys 25.6 / 21.1; 64 rows, two heads of 16000 keys 35.5 / 28.4; 256 rows, 8 heads
-// of 300 keys 8.8 / 17.0, of 1500 20.1 / 22.5; 500 rows, 8 heads of 700 keys 17.4 / 21.1.
+// of 300 keys 8.8 / 17.0, of 1500 20.1 / 22.5; 500 rows, 8 heads of 700 keys 17.4 / 21.1.  Around 640 tiles: 26 sequences of 32 rows, 8 heads (624) of 100 keys
+// 9.6 / 17.4, of 500 18.8 / 29.4; 500 rows, 500 keys, 16 heads (512) 16.0 / 22.3, 20 heads (640) 28.5 / 25.3.
 constexpr long long kIntTiles = 640, kIntKeys = 5 << 16, kIntLongest = 4096;
 bool cache_attn_int8_few(const heart_cache &c, int T, int Hq) {
   if (cache_attn_few(c.B, c.H, T, Hq)) return true;
@@ -761,8 +763,8 @@ bool cache_attn_int8_few(const heart_cache &c, int T, int Hq) {
 }
 // int8: a workgroup of sixteen wavefronts has a tile, whose keys (by the room of the page tables) are a slice of 4 KB for each at most:
 // nothing is divided, so no parts have to meet, and no loop.  One a CU.  us, divided (or four wavefronts) and so: one token of 1000 keys, two
-// heads of 64 11.3 / 8.9, 16 sequences of 64 keys, 8 heads 8.7 / 6.8, of 1000 14.5 / 10.5; 8 rows, 8 heads of 128, 480 keys 11.9 / 8.1; 32
-// sequences of 200 keys, 8 heads (384 items) 8.7 / 11.1.
+// heads of 64 11.3 / 8.9 (11.0 under any table with room for more than 1024), 16 sequences of 64 keys, 8 heads 8.7 / 6.8, of 1000
+// 14.5 / 10.5; 8 rows, 8 heads of 128, 480 keys 11.9 / 8.1; 32 sequences of 200 keys, 8 heads (384 items) 8.7 / 11.1.
 constexpr long long kFewAllItems = 256;
 static bool few_divides(int B, long long items) { return B <= kSplitSeqs && items <= kFewItems; }
 
