@@ -5,14 +5,14 @@
 // significant bits), so a quotient x / s is a half of an odd number or farther than 2^-12 of its size from one: computed to the last
 // bit it is rounded as the exact quotient is, and codes do not depend on how the division is done.
 //
-// A job is one page of a sequence that new tokens are in, one head, K or V: its rows, up to 16 KB of them, stay in registers
+// A job is one page of a sequence that new tokens are in, one head, K or V: its rows, up to 64 KB in four wavefronts, stay in registers
 // between their maximum and their codes, so each byte is moved once.  Where the page has tokens from before, its scale stays if it is
 // large enough; else their codes are divided anew, which is the only case that reads them.  The jobs of a sequence start at the
 // number  first / page + 2 b  (n tokens are in n / page + 2 pages at most), which every wavefront inverts on its own.
 //
 // Bound by memory, by latency where there are few tokens.  4680 tokens of 40 heads of 128 (144 MB in and out) 27 us, 5.3 TB/s (as a
 // copy of 512 MB), with one, two or four wavefronts for a page of 64 tokens alike; one token of each of 64 sequences 4.5.
-// Where all of their pages' scales grow it is as much in pages of 16 tokens, 3 more of 64, 17 more of 256 (8 heads: 33 MB read and written).
+// Where all of their pages' scales grow it is as much in pages of 16 tokens, 3 more of 64, 17 more of 256 (8 heads: 34 MB read, as much written).
 #include <type_traits>
 
 #include "cache_device.h"
